@@ -3,7 +3,7 @@
 Kinds of case:
   tree    `sp_tree_decode`, one layer's attention of a tree of drafted tokens per prompt over the joined cache
           [preamble; kept paths; response] and the tokens' own ancestors, with their K/V appended to the response cache
-  sample  `sp_sample`, a token for every row of logits (temperature, top-k, top-p, min-p, one given random number a row)
+  sample  `sp_sample`, a token for every row of logits (temperature, min-p, top-k, top-p, one given random number a row)
   accept  `sp_tree_accept`, the walk down the tree along the sampled tokens, and the accepted tokens' rows of all layers'
           response caches moved to where the next step expects them
 
@@ -418,12 +418,11 @@ def _plain_sample(s):
     rank = torch.arange(V, device=x.device)
     greedy = s.temperature[each] <= 0
     limit = torch.where(k > 0, k, V)
-    kept = rank < torch.where(greedy, 1, limit)[:, None]
+    kept = (w >= min_p[:, None]) & (rank < torch.where(greedy, 1, limit)[:, None])
     w = w * kept
     before = torch.cumsum(w, 1) - w
     total = before[:, -1:] + w[:, -1:]
     kept &= (before < top_p[:, None] * total) | (top_p >= 1)[:, None] | (rank == 0)
-    kept &= (w >= min_p[:, None]) | (rank == 0)
     w = w * kept
     run_mass = torch.cumsum(w, 1)
     at = (run_mass <= s.u.double()[:, None] * run_mass[:, -1:]).sum(1, keepdim=True)
@@ -517,12 +516,12 @@ def _exact_sample(s):
             continue
         order = np.argsort(-x, kind="stable")
         z = (x[order] - x[order[0]]) / T[i]
-        z = z[: int(k[i])] if 0 < k[i] < len(z) else z
         w = np.exp(z)
+        w = w[: int((w >= M[i]).sum())]
+        w = w[: int(k[i])] if k[i] > 0 else w
         if P[i] < 1:
             reached = np.searchsorted(np.cumsum(w), P[i] * w.sum())      # the first whose running mass is enough
             w = w[: max(1, min(len(w), reached + 1))]
-        w = w[: max(1, int((w >= M[i]).sum()))]
         mass = np.cumsum(w)
         j = min(int(np.searchsorted(mass, u[r] * mass[-1], side="right")), len(w) - 1)
         token[r], logprob[r] = order[j], z[j] - math.log(mass[-1])
