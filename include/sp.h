@@ -6,6 +6,8 @@
  *   - Bayesian path saliency from language-model logits       (Sec. 3.2.3, App. B.1 Eq. 2)
  *   - greedy top-k path pruning                               (Sec. 3.2.3, Alg. 3)
  *   - decode attention over the joined (pruned) KV cache      (Sec. 3.2.3, Alg. 3)
+ *   - the rest of the generation loop, several tokens a step: attention of a tree of drafted tokens over
+ *     that cache, the sampling of tokens, the acceptance of drafted ones
  *   - equilibrium position assignment (host helper)           (Sec. 3.2.2 Eq. 1, App. B.2)
  *
  * Conventions
@@ -240,6 +242,73 @@ sp_status sp_pruned_decode(sp_ctx *ctx, const sp_plan *plan, const int32_t *kept
                            int32_t resp_capacity, const int32_t *resp_len, int32_t resp_len_add,
                            const float *new_pos, const void *q_new, const void *k_new, const void *v_new,
                            void *o_out, float softmax_scale);
+
+/* ---- a5: attention of a tree of drafted tokens over the joined cache -------------------- */
+/*
+ * One step of several tokens for all prompts of the plan: node i of prompt b attends to
+ *   the joined cache of sp_pruned_decode  (+)  response cache rows [0, len_b)  (+)  its ancestors in the tree, and itself.
+ * A tree is what a small model drafts behind the last certain token (node 0), to be checked in one pass; without `parent` it is
+ * a chain, which is how a postamble or any other run of known tokens goes through in one call.
+ * The call first stores the nodes' K/V (and new_pos) at rows len_b + i of the response cache; rows beyond resp_capacity are
+ * dropped, not written.  The rows of nodes that are not there (i >= n_nodes[b]) are left as they are, in o_out too.
+ * parent: DEVICE int32 [n_prompts, max_nodes], the node above each node, which comes before it; -1: none.  NULL: the node before
+ *   (node 0: none).  Contract: -1 <= parent[i] < i; any other value is taken as -1.
+ * n_nodes: DEVICE int32 [n_prompts] or NULL (= max_nodes); clamped to [0, max_nodes].  max_nodes: 1 to 64
+ *   (SP_ERR_UNSUPPORTED above).
+ * new_pos: DEVICE fp32 [n_prompts, max_nodes]; q_new, o_out: DEVICE [n_prompts, max_nodes, n_q_heads, head_dim]; k_new, v_new:
+ *   DEVICE [n_prompts, max_nodes, n_kv_heads, head_dim]; all contiguous.  The others as in sp_pruned_decode.
+ */
+sp_status sp_tree_decode(sp_ctx *ctx, const sp_plan *plan, const int32_t *kept, int32_t k, const void *K_prefill,
+                         const void *V_prefill, int64_t kv_tok_stride, int64_t kv_head_stride, void *K_resp, void *V_resp,
+                         float *pos_resp, int32_t resp_capacity, const int32_t *resp_len, int32_t resp_len_add,
+                         const int32_t *parent, const int32_t *n_nodes, int32_t max_nodes, const float *new_pos,
+                         const void *q_new, const void *k_new, const void *v_new, void *o_out, float softmax_scale);
+
+/* ---- a6: sampling (Alg. 3, Sample) ------------------------------------------------------- */
+/*
+ * A token for every row of logits.  The tokens of a row are put in order: logit descending, ties by the lower index (as in
+ * sp_prune_topk).  Token v weighs exp((logits[r, v] - largest) / T).  Three filters, each applied to what the one before left,
+ * leave a prefix of the order:
+ *   min_p   the tokens that weigh at least min_p times the first one's weight   (off: <= 0 or NaN; above 1 counts as 1)
+ *   top_k   the first top_k tokens                                              (off: <= 0)
+ *   top_p   the shortest prefix that weighs at least top_p of what is left      (off: >= 1 or NaN; <= 0: the first token)
+ * token[r] is the first token of the order at which the running weight exceeds u[r] times the weight of what is left;
+ * logprob[r] the logarithm of its weight over that weight.  T <= 0 (or NaN): the first token of the order, logprob 0.
+ * Logits that are -inf or NaN take no part; a row with no others gets token -1 and logprob -inf.  Beside +inf nothing else weighs.
+ * logits: DEVICE [n_rows, vocab], row_stride in elements, dtype fp32 or bf16, base and rows 16-byte aligned; vocab at most 2^24
+ * (SP_ERR_UNSUPPORTED above).  u: DEVICE fp32 [n_rows], random numbers in [0, 1) from the caller (others are clamped to it,
+ * NaN counts as 0).  temperature, top_p, min_p: DEVICE fp32 and top_k: DEVICE int32, one value for every rows_per_set
+ * consecutive rows ([ceil(n_rows / rows_per_set)]: the settings of a prompt for all nodes of its tree), or NULL (T = 1,
+ * filter off).  token: DEVICE int32 [n_rows]; logprob: DEVICE fp32 [n_rows] or NULL.
+ * Weights are added up as 62-bit integers, so equal calls give equal tokens; a token that weighs less than 2^-38 of the first
+ * (2^-45 for 128256 tokens) may count as weightless.
+ */
+sp_status sp_sample(sp_ctx *ctx, const void *logits, sp_dtype dtype, int64_t n_rows, int64_t vocab, int64_t row_stride,
+                    int32_t rows_per_set, const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                    const float *u, int32_t *token, float *logprob);
+
+/* ---- a7: acceptance of drafted tokens ------------------------------------------------------ */
+/*
+ * Ends a step of drafted tokens.  For prompt b the walk begins at node 0 and goes from a node to its child (the lowest
+ * numbered, if several) whose drafted token equals what was sampled at the node, while there is one.  With tokens that
+ * sp_sample drew from the logits of every node the tokens along the walk are distributed as one-by-one generation's.
+ *   path[b, :]     the nodes of the walk in order, then -1        n_accepted[b]  how many they are
+ *   next_token[b]  what was sampled at the last of them (-1 without nodes): node 0 of the next step
+ *   resp_len_out[b] = len_b + n_accepted[b],  len_b = resp_len[b] + resp_len_add
+ * and row len_b + path[b, j] of the response caches (K, V of every layer, and pos_resp) moves to row len_b + j; rows from
+ * resp_len_out[b] on hold nothing of use afterwards, those of other prompts and below len_b are untouched.
+ * A node whose row lies beyond resp_capacity has no K/V and is not taken (nor is any behind it).
+ * draft, sampled: DEVICE int32 [n_prompts, max_nodes], the nodes' own tokens (node 0's is not read) and what was sampled at
+ * them (negative: nothing).  parent, n_nodes, max_nodes: as in sp_tree_decode.  K_resp, V_resp: DEVICE, n_layers blocks
+ * [n_prompts, resp_capacity, n_kv_heads, head_dim], layer_stride elements apart (at least a block; not read with one layer).
+ * pos_resp: DEVICE fp32 [n_prompts, resp_capacity] or NULL.  resp_len: DEVICE int32 [n_prompts] or NULL (= zeros).
+ * resp_len_out: DEVICE int32 [n_prompts], may be resp_len itself (one more, small, launch), not overlap it otherwise.
+ */
+sp_status sp_tree_accept(sp_ctx *ctx, int32_t n_prompts, int32_t max_nodes, const int32_t *parent, const int32_t *n_nodes,
+                         const int32_t *draft, const int32_t *sampled, sp_dtype dtype, int32_t n_layers, int64_t layer_stride,
+                         int32_t n_kv_heads, int32_t head_dim, void *K_resp, void *V_resp, float *pos_resp,
+                         int32_t resp_capacity, const int32_t *resp_len, int32_t resp_len_add, int32_t *path,
+                         int32_t *n_accepted, int32_t *next_token, int32_t *resp_len_out);
 
 /* ---- host helper: equilibrium positions (Sec. 3.2.2 Eq. 1; App. B.2 Eq. 3, Alg. 1) ----- */
 /*

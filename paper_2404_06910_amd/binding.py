@@ -71,6 +71,11 @@ def lib() -> C.CDLL:
         "sp_prune_topk": (C.c_int, [vp, vp, vp, i32, i32, i32, vp]),
         "sp_pruned_decode": (C.c_int, [vp, vp, vp, i32, vp, vp, i64, i64, vp, vp, vp, i32, vp, i32, vp, vp, vp, vp,
                                        vp, f32]),
+        "sp_tree_decode": (C.c_int, [vp, vp, vp, i32, vp, vp, i64, i64, vp, vp, vp, i32, vp, i32, vp, vp, i32, vp, vp, vp,
+                                     vp, vp, f32]),
+        "sp_sample": (C.c_int, [vp, vp, C.c_int, i64, i64, i64, i32, vp, vp, vp, vp, vp, vp, vp]),
+        "sp_tree_accept": (C.c_int, [vp, i32, i32, vp, vp, vp, vp, C.c_int, i32, i64, i32, i32, vp, vp, vp, i32, vp, i32,
+                                     vp, vp, vp, vp]),
         "sp_equilibrium_positions": (C.c_int, [C.POINTER(_SegTable), vp]),
     }
     for name, (res, args) in sig.items():
@@ -115,6 +120,25 @@ def _dev(t, what: str) -> int:
     if not t.is_cuda:
         raise ValueError("%s must be a CUDA tensor" % what)
     return t.data_ptr()
+
+
+def _table_dev(t, what: str, dtype: str, n: Optional[int]):
+    """Device pointer of a contiguous tensor of one 32-bit type (and size); None -> NULL."""
+    if t is None:
+        return None
+    if str(t.dtype) != dtype or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor" % (what, dtype))
+    if n is not None and t.numel() != n:
+        raise ValueError("%s has %d entries, expected %d" % (what, t.numel(), n))
+    return _dev(t, what)
+
+
+def _i32_dev(t, what: str, n: Optional[int] = None):
+    return _table_dev(t, what, "torch.int32", n)
+
+
+def _f32_dev(t, what: str, n: Optional[int] = None):
+    return _table_dev(t, what, "torch.float32", n)
 
 
 def _dtype_code(t) -> int:
@@ -221,6 +245,68 @@ class Context:
         if st != 0:
             self._check(st)
         return o_out
+
+    # -- a5 ------------------------------------------------------------------------------
+    def sp_tree_decode(self, plan: "Plan", kept, k: int, K_prefill, V_prefill, K_resp, V_resp, resp_capacity: int,
+                       q_new, k_new, v_new, o_out, softmax_scale: float, parent=None, n_nodes=None, resp_len=None,
+                       resp_len_add: int = 0, pos_resp=None, new_pos=None):
+        """q_new, o_out [n_prompts, max_nodes, n_q_heads, head_dim]; k_new, v_new [n_prompts, max_nodes, n_kv_heads, head_dim]."""
+        ks = K_prefill.stride()
+        if ks != V_prefill.stride() or ks[-1] != 1:
+            raise ValueError("K_prefill and V_prefill must share strides, inner stride 1")
+        B, N = q_new.shape[:2]
+        if q_new.dim() != 4 or B != plan.n_prompts or o_out.shape != q_new.shape:
+            raise ValueError("q_new and o_out must be [n_prompts, max_nodes, n_q_heads, head_dim]")
+        if k_new.shape[:2] != (B, N) or v_new.shape != k_new.shape:
+            raise ValueError("k_new and v_new must be [n_prompts, max_nodes, n_kv_heads, head_dim]")
+        for t, n in ((K_resp, "K_resp"), (V_resp, "V_resp"), (q_new, "q_new"), (k_new, "k_new"), (v_new, "v_new"), (o_out, "o_out")):
+            if not t.is_contiguous():
+                raise ValueError("%s must be contiguous" % n)
+            if _dtype_code(t) != plan.dtype:
+                raise ValueError("%s does not have the plan's dtype" % n)
+        self._check(lib().sp_tree_decode(
+            self._h, plan._h, _i32_dev(kept, "kept"), int(k), _dev(K_prefill, "K_prefill"), _dev(V_prefill, "V_prefill"),
+            ks[0], ks[1], _dev(K_resp, "K_resp"), _dev(V_resp, "V_resp"), _f32_dev(pos_resp, "pos_resp"), int(resp_capacity),
+            _i32_dev(resp_len, "resp_len", B), int(resp_len_add), _i32_dev(parent, "parent", B * N),
+            _i32_dev(n_nodes, "n_nodes", B), N, _f32_dev(new_pos, "new_pos", B * N), _dev(q_new, "q_new"), _dev(k_new, "k_new"),
+            _dev(v_new, "v_new"), _dev(o_out, "o_out"), float(softmax_scale)))
+        return o_out
+
+    # -- a6 ------------------------------------------------------------------------------
+    def sp_sample(self, logits, u, token, logprob=None, temperature=None, top_k=None, top_p=None, min_p=None,
+                  rows_per_set: int = 1):
+        if logits.dim() != 2 or logits.stride(1) != 1:
+            raise ValueError("logits must be [rows, vocab] with unit inner stride")
+        rows, per = logits.shape[0], int(rows_per_set)
+        sets = (rows + per - 1) // per if per > 0 else rows
+        self._check(lib().sp_sample(
+            self._h, _dev(logits, "logits"), _dtype_code(logits), rows, logits.shape[1], logits.stride(0), per,
+            _f32_dev(temperature, "temperature", sets), _i32_dev(top_k, "top_k", sets), _f32_dev(top_p, "top_p", sets),
+            _f32_dev(min_p, "min_p", sets), _f32_dev(u, "u", rows), _i32_dev(token, "token", rows),
+            _f32_dev(logprob, "logprob", rows)))
+        return token
+
+    # -- a7 ------------------------------------------------------------------------------
+    def sp_tree_accept(self, draft, sampled, K_resp, V_resp, path, n_accepted, next_token, resp_len_out, parent=None,
+                       n_nodes=None, resp_len=None, resp_len_add: int = 0, pos_resp=None):
+        """K_resp, V_resp: [n_layers,] n_prompts, resp_capacity, n_kv_heads, head_dim, every layer's block contiguous."""
+        B, N = draft.shape
+        if K_resp.dim() not in (4, 5) or K_resp.shape[-4] != B or V_resp.shape != K_resp.shape or V_resp.stride() != K_resp.stride():
+            raise ValueError("K_resp and V_resp must be alike, [n_layers,] n_prompts, resp_capacity, n_kv_heads, head_dim")
+        block = K_resp[0] if K_resp.dim() == 5 else K_resp
+        if not block.is_contiguous():
+            raise ValueError("a layer's block of K_resp and V_resp must be contiguous")
+        if _dtype_code(V_resp) != _dtype_code(K_resp):
+            raise ValueError("K_resp and V_resp must have one dtype")
+        layers, stride = (K_resp.shape[0], K_resp.stride(0)) if K_resp.dim() == 5 else (1, 0)
+        cap, heads, d = block.shape[1:]
+        self._check(lib().sp_tree_accept(
+            self._h, B, N, _i32_dev(parent, "parent", B * N), _i32_dev(n_nodes, "n_nodes", B), _i32_dev(draft, "draft", B * N),
+            _i32_dev(sampled, "sampled", B * N), _dtype_code(K_resp), layers, stride, heads, d, _dev(K_resp, "K_resp"),
+            _dev(V_resp, "V_resp"), _f32_dev(pos_resp, "pos_resp", B * cap), cap, _i32_dev(resp_len, "resp_len", B),
+            int(resp_len_add), _i32_dev(path, "path", B * N), _i32_dev(n_accepted, "n_accepted", B),
+            _i32_dev(next_token, "next_token", B), _i32_dev(resp_len_out, "resp_len_out", B)))
+        return path
 
 
 class Plan:

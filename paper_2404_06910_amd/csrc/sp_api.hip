@@ -1311,13 +1311,11 @@ extern "C" sp_status sp_prune_topk(sp_ctx *ctx, const float *score, const int32_
 // ---------------------------------------------------------------------------------------
 // a4 decode
 // ---------------------------------------------------------------------------------------
-extern "C" sp_status sp_pruned_decode(sp_ctx *ctx, const sp_plan *plan, const int32_t *kept, int32_t k,
-                                      const void *K_prefill, const void *V_prefill, int64_t kv_tok_stride,
-                                      int64_t kv_head_stride, void *K_resp, void *V_resp, float *pos_resp,
-                                      int32_t resp_capacity, const int32_t *resp_len, int32_t resp_len_add,
-                                      const float *new_pos, const void *q_new, const void *k_new,
-                                      const void *v_new, void *o_out, float softmax_scale) {
-  if (!ctx) return fail(nullptr, SP_ERR_INVALID_ARG, "ctx is NULL");
+static sp_status check_decode_args(sp_ctx *ctx, const sp_plan *plan, const int32_t *kept, int32_t k, const void *K_prefill,
+                                   const void *V_prefill, int64_t kv_tok_stride, int64_t kv_head_stride, const void *K_resp,
+                                   const void *V_resp, const float *pos_resp, int32_t resp_capacity, int32_t resp_len_add,
+                                   const float *new_pos, const void *q_new, const void *k_new, const void *v_new, const void *o_out,
+                                   float softmax_scale) {
   if (!plan || !K_prefill || !V_prefill || !K_resp || !V_resp || !q_new || !k_new || !v_new || !o_out)
     return fail(&ctx->err, SP_ERR_INVALID_ARG, "NULL argument");
   if (plan->ctx != ctx) return fail(&ctx->err, SP_ERR_INVALID_ARG, "plan was not created on this context");
@@ -1341,11 +1339,115 @@ extern "C" sp_status sp_pruned_decode(sp_ctx *ctx, const sp_plan *plan, const in
     worst = std::max(worst, plan->shared_rng_end[b] - plan->shared_rng_beg[b] + int64_t(k) * plan->path_max_ranges[b]);
   if (worst > 120)
     return fail(&ctx->err, SP_ERR_UNSUPPORTED, "joined cache has %lld disjoint ranges (limit 120)", (long long)worst);
+  return SP_OK;
+}
+
+extern "C" sp_status sp_pruned_decode(sp_ctx *ctx, const sp_plan *plan, const int32_t *kept, int32_t k,
+                                      const void *K_prefill, const void *V_prefill, int64_t kv_tok_stride,
+                                      int64_t kv_head_stride, void *K_resp, void *V_resp, float *pos_resp,
+                                      int32_t resp_capacity, const int32_t *resp_len, int32_t resp_len_add,
+                                      const float *new_pos, const void *q_new, const void *k_new,
+                                      const void *v_new, void *o_out, float softmax_scale) {
+  if (!ctx) return fail(nullptr, SP_ERR_INVALID_ARG, "ctx is NULL");
+  const sp_status st = check_decode_args(ctx, plan, kept, k, K_prefill, V_prefill, kv_tok_stride, kv_head_stride, K_resp, V_resp,
+                                         pos_resp, resp_capacity, resp_len_add, new_pos, q_new, k_new, v_new, o_out, softmax_scale);
+  if (st != SP_OK) return st;
   sp::DecodeArgs a{kept, k, K_prefill, V_prefill, kv_tok_stride, kv_head_stride, K_resp, V_resp, pos_resp,
                    resp_capacity, resp_len, resp_len_add, new_pos, q_new, k_new, v_new, o_out, softmax_scale};
   SP_HIP(ctx, hipSetDevice(ctx->device));
   hipError_t e = sp::launch_decode(plan, a, ctx->stream);
   if (e != hipSuccess) return fail(&ctx->err, SP_ERR_HIP, "decode launch: %s", hipGetErrorString(e));
+  return SP_OK;
+}
+
+// ---------------------------------------------------------------------------------------
+// a5 tree decode
+// ---------------------------------------------------------------------------------------
+extern "C" sp_status sp_tree_decode(sp_ctx *ctx, const sp_plan *plan, const int32_t *kept, int32_t k, const void *K_prefill,
+                                    const void *V_prefill, int64_t kv_tok_stride, int64_t kv_head_stride, void *K_resp,
+                                    void *V_resp, float *pos_resp, int32_t resp_capacity, const int32_t *resp_len,
+                                    int32_t resp_len_add, const int32_t *parent, const int32_t *n_nodes, int32_t max_nodes,
+                                    const float *new_pos, const void *q_new, const void *k_new, const void *v_new, void *o_out,
+                                    float softmax_scale) {
+  if (!ctx) return fail(nullptr, SP_ERR_INVALID_ARG, "ctx is NULL");
+  const sp_status st = check_decode_args(ctx, plan, kept, k, K_prefill, V_prefill, kv_tok_stride, kv_head_stride, K_resp, V_resp,
+                                         pos_resp, resp_capacity, resp_len_add, new_pos, q_new, k_new, v_new, o_out, softmax_scale);
+  if (st != SP_OK) return st;
+  if (max_nodes <= 0) return fail(&ctx->err, SP_ERR_INVALID_ARG, "max_nodes must be positive");
+  if (max_nodes > sp::kMaxNodes)
+    return fail(&ctx->err, SP_ERR_UNSUPPORTED, "%d nodes (limit %d)", max_nodes, sp::kMaxNodes);
+  if (int64_t(plan->n_prompts) * max_nodes > INT32_MAX)
+    return fail(&ctx->err, SP_ERR_UNSUPPORTED, "n_prompts * max_nodes does not fit 31 bits");
+  if (o_out == q_new || o_out == k_new || o_out == v_new)
+    return fail(&ctx->err, SP_ERR_INVALID_ARG, "o_out must not alias an input");
+  SP_HIP(ctx, hipSetDevice(ctx->device));
+  hipError_t e = sp::launch_tree_decode(
+      plan, sp::TreeArgs{kept, k, K_prefill, V_prefill, kv_tok_stride, kv_head_stride, K_resp, V_resp, pos_resp, resp_capacity, resp_len,
+                         resp_len_add, parent, n_nodes, max_nodes, new_pos, q_new, k_new, v_new, o_out, softmax_scale, 0},
+      ctx->stream);
+  if (e != hipSuccess) return fail(&ctx->err, SP_ERR_HIP, "tree decode launch: %s", hipGetErrorString(e));
+  return SP_OK;
+}
+
+// ---------------------------------------------------------------------------------------
+// a6 sampling
+// ---------------------------------------------------------------------------------------
+extern "C" sp_status sp_sample(sp_ctx *ctx, const void *logits, sp_dtype dtype, int64_t n_rows, int64_t vocab, int64_t row_stride,
+                               int32_t rows_per_set, const float *temperature, const int32_t *top_k, const float *top_p,
+                               const float *min_p, const float *u, int32_t *token, float *logprob) {
+  if (!ctx) return fail(nullptr, SP_ERR_INVALID_ARG, "ctx is NULL");
+  if (n_rows < 0 || vocab <= 0 || rows_per_set <= 0 || row_stride < vocab)
+    return fail(&ctx->err, SP_ERR_INVALID_ARG, "bad sizes (n_rows >= 0, vocab > 0, rows_per_set > 0, row_stride >= vocab)");
+  if (n_rows == 0) return SP_OK;
+  if (!logits || !u || !token) return fail(&ctx->err, SP_ERR_INVALID_ARG, "NULL argument");
+  if (dtype != SP_F32 && dtype != SP_BF16) return fail(&ctx->err, SP_ERR_INVALID_ARG, "unknown dtype");
+  if (n_rows > (int64_t(1) << 30)) return fail(&ctx->err, SP_ERR_UNSUPPORTED, "n_rows above 2^30");
+  if (vocab > sp::kSampleMaxVocab) return fail(&ctx->err, SP_ERR_UNSUPPORTED, "vocab above 2^24");
+  const int64_t esz = dtype == SP_BF16 ? 2 : 4;
+  if ((reinterpret_cast<uintptr_t>(logits) & 15) || (row_stride * esz) % 16)
+    return fail(&ctx->err, SP_ERR_UNSUPPORTED, "logits base and row stride must be 16-byte aligned");
+  SP_HIP(ctx, hipSetDevice(ctx->device));
+  hipError_t e = sp::launch_sample(
+      sp::SampleArgs{logits, vocab, row_stride, rows_per_set, temperature, top_k, top_p, min_p, u, token, logprob}, dtype, n_rows,
+      ctx->stream);
+  if (e != hipSuccess) return fail(&ctx->err, SP_ERR_HIP, "sample launch: %s", hipGetErrorString(e));
+  return SP_OK;
+}
+
+// ---------------------------------------------------------------------------------------
+// a7 acceptance
+// ---------------------------------------------------------------------------------------
+extern "C" sp_status sp_tree_accept(sp_ctx *ctx, int32_t n_prompts, int32_t max_nodes, const int32_t *parent, const int32_t *n_nodes,
+                                    const int32_t *draft, const int32_t *sampled, sp_dtype dtype, int32_t n_layers,
+                                    int64_t layer_stride, int32_t n_kv_heads, int32_t head_dim, void *K_resp, void *V_resp,
+                                    float *pos_resp, int32_t resp_capacity, const int32_t *resp_len, int32_t resp_len_add,
+                                    int32_t *path, int32_t *n_accepted, int32_t *next_token, int32_t *resp_len_out) {
+  if (!ctx) return fail(nullptr, SP_ERR_INVALID_ARG, "ctx is NULL");
+  if (!draft || !sampled || !K_resp || !V_resp || !path || !n_accepted || !next_token || !resp_len_out)
+    return fail(&ctx->err, SP_ERR_INVALID_ARG, "NULL argument");
+  if (n_prompts <= 0 || max_nodes <= 0 || n_layers <= 0 || n_kv_heads <= 0 || resp_capacity <= 0 || resp_len_add < 0)
+    return fail(&ctx->err, SP_ERR_INVALID_ARG, "bad sizes (n_prompts, max_nodes, n_layers, n_kv_heads, resp_capacity > 0, resp_len_add >= 0)");
+  if (dtype != SP_F32 && dtype != SP_BF16) return fail(&ctx->err, SP_ERR_INVALID_ARG, "unknown dtype");
+  if (head_dim != 64 && head_dim != 128) return fail(&ctx->err, SP_ERR_UNSUPPORTED, "head_dim %d (64 or 128)", head_dim);
+  if (max_nodes > sp::kMaxNodes)
+    return fail(&ctx->err, SP_ERR_UNSUPPORTED, "%d nodes (limit %d)", max_nodes, sp::kMaxNodes);
+  if (n_layers > 32767 || n_kv_heads > 65535) return fail(&ctx->err, SP_ERR_UNSUPPORTED, "more than 32767 layers or 65535 KV heads");
+  const int64_t esz = dtype == SP_BF16 ? 2 : 4, row = int64_t(n_kv_heads) * head_dim;
+  const int64_t align = 16 / esz;
+  if (n_layers > 1 && layer_stride / row / resp_capacity < n_prompts)
+    return fail(&ctx->err, SP_ERR_INVALID_ARG, "layer_stride smaller than a layer's block");
+  if (n_layers > 1 && layer_stride % align)
+    return fail(&ctx->err, SP_ERR_UNSUPPORTED, "layer_stride must be a multiple of %lld elements", (long long)align);
+  if ((reinterpret_cast<uintptr_t>(K_resp) | reinterpret_cast<uintptr_t>(V_resp)) & 15)
+    return fail(&ctx->err, SP_ERR_UNSUPPORTED, "K_resp, V_resp must be 16-byte aligned");
+  if (resp_len && resp_len != resp_len_out && resp_len < resp_len_out + n_prompts && resp_len_out < resp_len + n_prompts)
+    return fail(&ctx->err, SP_ERR_INVALID_ARG, "resp_len_out overlaps resp_len");
+  SP_HIP(ctx, hipSetDevice(ctx->device));
+  hipError_t e = sp::launch_accept(
+      sp::AcceptArgs{parent, n_nodes, draft, sampled, max_nodes, K_resp, V_resp, pos_resp, n_layers > 1 ? layer_stride * esz : 0,
+                     int32_t(row * esz), resp_capacity, resp_len, resp_len_add, path, n_accepted, next_token, resp_len_out},
+      n_prompts, n_layers, ctx->stream);
+  if (e != hipSuccess) return fail(&ctx->err, SP_ERR_HIP, "accept launch: %s", hipGetErrorString(e));
   return SP_OK;
 }
 

@@ -276,4 +276,52 @@ void decode_scratch(const sp_plan *plan, int n_cu, size_t *part_bytes, size_t *c
 const DecodeRegion *decode_region(const sp_plan *plan, hipStream_t s);
 hipError_t launch_decode(const sp_plan *plan, const DecodeArgs &a, hipStream_t s);
 
+constexpr int kMaxNodes = 64;           // of a tree of drafted tokens: a bit mask, a lane each
+struct TreeArgs {
+  const int32_t *kept;
+  int32_t k;
+  const void *Kp, *Vp;
+  int64_t kv_tok_stride, kv_head_stride;
+  void *Kr, *Vr;
+  float *pos_resp;
+  int32_t resp_capacity;
+  const int32_t *resp_len;
+  int32_t resp_len_add;
+  const int32_t *parent, *n_nodes;
+  int32_t max_nodes;
+  const float *new_pos;
+  const void *q_new, *k_new, *v_new;
+  void *o_out;
+  float scale;
+  int32_t few_wgs;                      // see build_key_table
+};
+hipError_t launch_tree_decode(const sp_plan *plan, TreeArgs a, hipStream_t s);
+
+struct SampleArgs {
+  const void *logits;
+  int64_t vocab, row_stride;
+  int32_t rows_per_set;
+  const float *temperature;
+  const int32_t *top_k;
+  const float *top_p, *min_p, *u;
+  int32_t *token;
+  float *logprob;
+};
+constexpr int64_t kSampleMaxVocab = int64_t(1) << 24;
+hipError_t launch_sample(const SampleArgs &a, sp_dtype dtype, int64_t n_rows, hipStream_t s);
+
+struct AcceptArgs {
+  const int32_t *parent, *n_nodes, *draft, *sampled;
+  int32_t max_nodes;
+  void *Kr, *Vr;
+  float *pos_resp;
+  int64_t layer_bytes;
+  int32_t row_bytes;                    // of a token: all KV heads
+  int32_t resp_capacity;
+  const int32_t *resp_len;
+  int32_t resp_len_add;
+  int32_t *path, *n_accepted, *next_token, *resp_len_out;
+};
+hipError_t launch_accept(const AcceptArgs &a, int32_t n_prompts, int32_t n_layers, hipStream_t s);
+
 }  // namespace sp

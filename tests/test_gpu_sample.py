@@ -1,0 +1,267 @@
+"""sp_sample against the 64-bit oracle.  Tokens are equal wherever the oracle's decision is further from its border than the
+weights' resolution: a weight is off by 2^-(62 - b) of the largest, b bits of the vocabulary, a sum of all by 2^(2 b - 62) at most
+(four times that is asked for, and at least 2^-45, where the oracle's own sums of doubles end)."""
+import numpy as np
+import pytest
+import torch
+
+import sp_synth
+from oracle import sp_oracle_tree as ort
+from paper_2404_06910_amd import binding as B
+
+from gpu_util import TORCH_DT, dev
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = B.Context(0)
+    yield c
+    c.close()
+
+
+def _sample(ctx, x, u, dtype, pitch=0, rows_per_set=1, **sets):
+    """x [rows, vocab] fp32 as stored"""
+    rows, vocab = x.shape
+    per = 8 if dtype == "bf16" else 4
+    full = torch.full((rows, (vocab + per - 1) // per * per + pitch), float("inf"), dtype=TORCH_DT[dtype], device="cuda")
+    full[:, :vocab] = dev(x, dtype)
+    token = torch.full((rows,), -7, dtype=torch.int32, device="cuda")
+    logprob = torch.full((rows,), 7.0, device="cuda")
+    kw = {n: None if a is None else dev(a) for n, a in sets.items()}
+    ctx.sp_sample(full[:, :vocab], dev(np.asarray(u, np.float32)), token, logprob=logprob, rows_per_set=rows_per_set, **kw)
+    torch.cuda.synchronize()
+    return token.cpu().numpy(), logprob.cpu().numpy()
+
+
+def _check(x, u, got, rows_per_set=1, least_sure=0.9, **sets):
+    token, logprob = got
+    bits = max(1, int(x.shape[1] - 1).bit_length())
+    fine = max(2.0 ** (2 * bits - 60), 2.0 ** -45)
+    sure = 0
+    for r in range(len(x)):
+        args = {n: a[r // rows_per_set] for n, a in sets.items() if a is not None}
+        want, lp, margin = ort.sample_row(x[r], u[r], **args)
+        if margin > fine:
+            sure += 1
+            assert token[r] == want, (r, args, u[r], token[r], want, margin)
+            # the quotient's logarithm in 64 bits from weights of that resolution, then one rounding to 32
+            if np.isfinite(lp):
+                assert abs(logprob[r] - lp) <= 2.0 ** -24 * abs(lp) + fine, (r, logprob[r], lp)
+            else:
+                assert logprob[r] == lp
+    assert sure >= least_sure * len(x)
+
+
+def _params(rng, n):
+    f = lambda a: np.asarray(a, np.float32)
+    on = rng.integers(0, 2, (4, n)).astype(bool)
+    return dict(temperature=f(np.where(on[0], rng.uniform(0.3, 2.5, n), 1.0) * (rng.random(n) > 0.1)),
+                top_k=np.where(on[1], rng.integers(1, 60, n), rng.choice([0, -3, 1 << 30], n)).astype(np.int32),
+                top_p=f(np.where(on[2], rng.uniform(0.05, 0.99, n), 1.0)), min_p=f(np.where(on[3], rng.uniform(0.001, 0.5, n), 0.0)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [1, 2, 3, 7, 8, 9, 63, 100, 512, 1000, 4099, 8191, 32000, 50257, 128256])
+@pytest.mark.parametrize("std", [0.3, 3.0])
+def test_vocabularies_and_filters(ctx, dtype, vocab, std):
+    rng = np.random.default_rng(vocab)
+    rows = 24 if vocab > 20000 else 64
+    x = sp_synth.round_to_dtype(rng.standard_normal((rows, vocab), dtype=np.float32) * np.float32(std), dtype)
+    u = rng.random(rows).astype(np.float32)
+    sets = _params(rng, rows)
+    print("case:", dtype, vocab, std, flush=True)
+    _check(x, u, _sample(ctx, x, u, dtype, pitch=16, **sets), **sets)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("what", ["equal", "two_values", "narrow", "wide", "masked_lowest", "masked_inf", "tiny", "negative", "zeros_of_both_signs"])
+@pytest.mark.parametrize("vocab", [130, 9000, 70001])
+def test_distributions(ctx, dtype, what, vocab):
+    """many equal values, values of one first-level bin, masks of the lowest value"""
+    rng = np.random.default_rng(len(what) * vocab)
+    rows = 12
+    x = rng.standard_normal((rows, vocab)).astype(np.float32)
+    if what == "equal":
+        x[:] = 1.5
+    elif what == "two_values":
+        x = np.where(x > 0, np.float32(2.0), np.float32(1.0))
+    elif what == "narrow":
+        x = np.float32(5.0) + x * np.float32(1e-3)
+    elif what == "wide":
+        x *= 200
+    elif what == "masked_lowest":
+        x[:, 5:-5] = np.finfo(np.float32).min if dtype == "f32" else -3.3895313892515355e38
+    elif what == "masked_inf":
+        x[:, rng.random(vocab) < 0.9] = -np.inf
+    elif what == "tiny":
+        x *= np.float32(1e-30)
+    elif what == "negative":
+        x -= 40
+    else:
+        x = np.where(x > 0, np.float32(0.0), np.float32(-0.0))
+    x = sp_synth.round_to_dtype(x, dtype)
+    u = rng.random(rows).astype(np.float32)
+    sets = _params(rng, rows)
+    print("case:", dtype, what, vocab, flush=True)
+    # with equal weights every border is a multiple of a weight, and half of the draws of a cut may lie on one
+    _check(x, u, _sample(ctx, x, u, dtype, **sets), least_sure=0.5, **sets)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_values_that_are_no_numbers(ctx, dtype):
+    inf, nan = np.inf, np.nan
+    x = np.zeros((9, 40), np.float32)
+    x[0] = -inf
+    x[1] = nan
+    x[2, ::2], x[2, 1::2] = nan, -inf
+    x[3] = -inf; x[3, 17] = -3.0
+    x[4, [5, 9]] = inf
+    x[5, 3] = nan; x[5, 4] = 9.0
+    x[6, 39] = inf; x[6, 0] = nan
+    x[7] = nan; x[7, 39] = -3.3895313892515355e38
+    x[8] = -inf; x[8, :2] = -3.3895313892515355e38
+    x = sp_synth.round_to_dtype(x, dtype)
+    for T in (1.0, 0.0, np.inf, 1e-30, 1e30, nan, -1.0):
+        for u in (0.0, 0.4, 0.9999):
+            sets = dict(temperature=np.full(9, T, np.float32))
+            got = _sample(ctx, x, np.full(9, u, np.float32), dtype, **sets)
+            print("case:", dtype, T, u, flush=True)
+            _check(x, np.full(9, u, np.float32), got, least_sure=0.5, **sets)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_borders_of_the_settings(ctx, dtype):
+    """u at and beyond its ends, settings that are off, everything and nothing kept"""
+    rng = np.random.default_rng(4)
+    x = sp_synth.round_to_dtype(rng.standard_normal((1, 600)).astype(np.float32), dtype)
+    order = ort.sample_order(x[0])
+    nan = np.nan
+    for u, sets, want in [
+            (0.0, {}, order[0]), (nan, {}, order[0]), (-5.0, {}, order[0]),
+            (1.0, dict(top_k=7), order[6]), (0.99999994, dict(top_k=7), order[6]), (9.0, dict(top_k=600), order[599]),
+            (1.0, dict(top_k=601), order[599]), (1.0, dict(top_p=0.0), order[0]), (1.0, dict(top_p=-1.0), order[0]),
+            (1.0, dict(top_p=1e-20), order[0]), (1.0, dict(min_p=1.0), order[0]), (1.0, dict(min_p=3.0), order[0]),
+            (1.0, dict(min_p=nan, top_p=nan, top_k=0), order[599]), (1.0, dict(min_p=-1.0, top_p=2.0, top_k=-1), order[599]),
+            (0.7, dict(temperature=0.0, top_k=5), order[0]), (0.7, dict(top_k=1, top_p=0.5, min_p=0.1), order[0])]:
+        arrays = {n: np.array([v], np.int32 if n == "top_k" else np.float32) for n, v in sets.items()}
+        got = _sample(ctx, x, [u], dtype, **arrays)
+        print("case:", dtype, u, sets, flush=True)
+        assert got[0][0] == want, (u, sets)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_draws_follow_the_order(ctx, dtype):
+    """rows of one distribution with u over [0, 1): the tokens come in order, as often as they weigh"""
+    rng = np.random.default_rng(5)
+    n, vocab = 2000, 50
+    row = sp_synth.round_to_dtype(rng.standard_normal(vocab).astype(np.float32), dtype)
+    u = ((np.arange(n) + 0.5) / n).astype(np.float32)
+    token, logprob = _sample(ctx, np.tile(row, (n, 1)), u, dtype)
+    order = list(ort.sample_order(row))
+    place = [order.index(t) for t in token]
+    assert place == sorted(place)
+    w = np.exp(row.astype(np.float64))
+    got = np.bincount(token, minlength=vocab) / n
+    np.testing.assert_allclose(got, w / w.sum(), atol=1.01 / n)
+    np.testing.assert_allclose(logprob, np.log(w / w.sum())[token], rtol=2.0 ** -23)
+
+
+@pytest.mark.parametrize("rows,per", [(1, 1), (7, 3), (64, 16), (300, 300), (5, 100)])
+def test_settings_of_several_rows(ctx, rows, per):
+    rng = np.random.default_rng(rows)
+    x = sp_synth.round_to_dtype(rng.standard_normal((rows, 777), dtype=np.float32) * 2, "bf16")
+    u = rng.random(rows).astype(np.float32)
+    sets = _params(rng, (rows + per - 1) // per)
+    _check(x, u, _sample(ctx, x, u, "bf16", rows_per_set=per, **sets), rows_per_set=per, **sets)
+
+
+def test_many_rows_equal_calls_and_graphs(ctx):
+    rng = np.random.default_rng(6)
+    rows, vocab = 700, 3001
+    x = sp_synth.round_to_dtype(rng.standard_normal((rows, vocab), dtype=np.float32) * 2, "bf16")
+    u = rng.random(rows).astype(np.float32)
+    sets = _params(rng, rows)
+    first = _sample(ctx, x, u, "bf16", **sets)
+    _check(x, u, first, **sets)
+    L = torch.zeros((rows, 3008), dtype=torch.bfloat16, device="cuda")
+    L[:, :vocab] = dev(x, "bf16")
+    U, kw = dev(u), {n: dev(a) for n, a in sets.items()}
+    token, logprob = torch.zeros(rows, dtype=torch.int32, device="cuda"), torch.zeros(rows, device="cuda")
+    main = torch.cuda.current_stream().cuda_stream
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        ctx.sp_set_stream(torch.cuda.current_stream().cuda_stream)
+        ctx.sp_sample(L[:, :vocab], U, token, logprob=logprob, **kw)
+    ctx.sp_set_stream(main)
+    for rep in range(4):
+        if rep:
+            L[:, :vocab] = L[:, :vocab].flip(0)
+            U.copy_(U.flip(0))
+        want, wlp = torch.zeros_like(token), torch.zeros_like(logprob)
+        ctx.sp_sample(L[:, :vocab], U, want, logprob=wlp, **kw)
+        token.fill_(-9)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(token, want) and torch.equal(logprob, wlp)
+        if rep == 0:
+            assert np.array_equal(token.cpu().numpy(), first[0])
+
+
+def test_without_logprob_and_on_another_stream(ctx):
+    rng = np.random.default_rng(7)
+    x = torch.from_numpy(rng.standard_normal((5, 64)).astype(np.float32)).cuda()
+    u = torch.rand(5, device="cuda")
+    a, b = (torch.full((5,), -1, dtype=torch.int32, device="cuda") for _ in range(2))
+    ctx.sp_sample(x, u, a)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    main = torch.cuda.current_stream().cuda_stream
+    ctx.sp_set_stream(s.cuda_stream)
+    ctx.sp_sample(x, u, b)
+    ctx.sp_set_stream(main)
+    torch.cuda.synchronize()
+    assert torch.equal(a, b) and (a >= 0).all()
+
+
+def test_rows_behind_4_gb(ctx):
+    vocab = 1000
+    pitch = (1 << 31) + 1024                                # elements from one row to the next
+    flat = torch.empty(pitch * 2 + 1000, dtype=torch.bfloat16, device="cuda")
+    x = torch.as_strided(flat, (3, vocab), (pitch, 1))
+    rng = np.random.default_rng(8)
+    host = sp_synth.round_to_dtype(rng.standard_normal((3, vocab)).astype(np.float32), "bf16")
+    x.copy_(dev(host, "bf16"))
+    u = np.array([0.2, 0.5, 0.8], np.float32)
+    token = torch.zeros(3, dtype=torch.int32, device="cuda")
+    ctx.sp_sample(x, dev(u), token)
+    torch.cuda.synchronize()
+    assert list(token.cpu().numpy()) == [ort.sample_row(host[r], u[r])[0] for r in range(3)]
+
+
+def test_refusals(ctx):
+    x = torch.zeros((4, 64), device="cuda")
+    u = torch.zeros(4, device="cuda")
+    token = torch.full((4,), -7, dtype=torch.int32, device="cuda")
+
+    def status(logits=x, u=u, token=token, **kw):
+        with pytest.raises((B.SpError, ValueError)) as e:
+            ctx.sp_sample(logits, u, token, **kw)
+        return getattr(e.value, "status", None)
+
+    odd = torch.zeros((4, 68), device="cuda")
+    assert status(logits=odd[:, 1:65]) == -3                 # base
+    assert status(logits=torch.zeros((4, 66), device="cuda")[:, :64]) == -3
+    assert status(rows_per_set=0) == -1
+    assert status(logits=torch.as_strided(torch.zeros(1 << 20, device="cuda"), (4, 64), (32, 1))) == -1
+    assert status(logits=x.half()) is None
+    long = torch.zeros((1, (1 << 24) + 4), dtype=torch.bfloat16, device="cuda")
+    assert status(logits=long, u=u[:1], token=token[:1]) == -3
+    assert status(u=u[:3]) is None and status(u=u.double()) is None and status(token=token.long()) is None
+    assert status(top_k=torch.zeros(4, device="cuda")) is None and status(temperature=u[:2]) is None
+    assert status(logits=x.cpu()) is None and status(logits=x.t()) is None
+    ctx.sp_sample(x[:0], u[:0], token[:0])                   # no rows: nothing to do
+    torch.cuda.synchronize()
+    assert (token == -7).all()
