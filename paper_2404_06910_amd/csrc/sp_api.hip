@@ -165,6 +165,7 @@ extern "C" sp_status sp_create(sp_ctx **out, int device, void *hip_stream) {
 static void ctx_unref(sp_ctx *ctx) {
   if (--ctx->refs) return;
   for (void *p : ctx->dec_chunks) (void)hipFree(p);
+  for (void *p : ctx->tree_free) (void)hipFree(p);
   delete ctx;
 }
 
@@ -239,41 +240,77 @@ static bool more_decode_regions(const sp_plan *p) {
   return true;
 }
 
-// The region of the order of execution that a launch on `s` joins.  Errors are dealt with here: the launch that follows
-// reports its own.
-const sp::DecodeRegion *sp::decode_region(const sp_plan *p, hipStream_t s) {
-  if (p->dec_regions.empty()) return nullptr;
+// The order of execution that a launch on `s` joins: a stream (hipStreamPerThread: of one thread), or a stream within one capture.
+// False if it cannot be told; errors are dealt with here: the launch that follows reports its own.
+static bool execution_order(hipStream_t s, sp::DecodeRegion *who) {
   static std::atomic<unsigned long long> threads{0};
   thread_local const unsigned long long this_thread = ++threads;
-  const unsigned long long thread = s == hipStreamPerThread ? this_thread : 0;   // that name is another stream in every thread
-  unsigned long long capture = 0;
+  who->stream = s;
+  who->thread = s == hipStreamPerThread ? this_thread : 0;   // that name is another stream in every thread
+  who->capture = 0;
   if (s) {                                              // the null stream cannot be captured
     hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
     unsigned long long id = 0;
     if (hipStreamGetCaptureInfo(s, &st, &id) != hipSuccess) {
       (void)hipGetLastError();
-      return nullptr;
+      return false;
     }
-    if (st != hipStreamCaptureStatusNone) capture = id + 1;
+    if (st != hipStreamCaptureStatusNone) who->capture = id + 1;
   }
-  DecodeRegion *unused = nullptr;
-  for (DecodeRegion &r : p->dec_regions) {
-    if (r.taken && r.stream == s && r.capture == capture && r.thread == thread) return &r;
+  return true;
+}
+
+// Of some regions the one that belongs to `who`, or one that is free and now does, or nullptr.
+static sp::DecodeRegion *region_of(std::vector<sp::DecodeRegion> &regions, const sp::DecodeRegion &who) {
+  sp::DecodeRegion *unused = nullptr;
+  for (sp::DecodeRegion &r : regions) {
+    if (r.taken && r.stream == who.stream && r.capture == who.capture && r.thread == who.thread) return &r;
     if (!r.taken && !unused) unused = &r;
   }
-  if (!unused) {
-    const size_t have = p->dec_regions.size();
-    if (!more_decode_regions(p)) {
-      (void)hipGetLastError();
-      return nullptr;
-    }
-    unused = &p->dec_regions[have];
+  if (unused) {
+    unused->stream = who.stream;
+    unused->capture = who.capture;
+    unused->thread = who.thread;
+    unused->taken = true;
   }
-  unused->stream = s;
-  unused->capture = capture;
-  unused->thread = thread;
-  unused->taken = true;
   return unused;
+}
+
+const sp::DecodeRegion *sp::decode_region(const sp_plan *p, hipStream_t s) {
+  DecodeRegion who{};
+  if (p->dec_regions.empty() || !execution_order(s, &who)) return nullptr;
+  if (DecodeRegion *r = region_of(p->dec_regions, who)) return r;
+  if (!more_decode_regions(p)) {
+    (void)hipGetLastError();
+    return nullptr;
+  }
+  return region_of(p->dec_regions, who);
+}
+
+void *sp::tree_scratch(const sp_plan *p, hipStream_t s) {
+  DecodeRegion who{};
+  if (!execution_order(s, &who)) return nullptr;
+  if (DecodeRegion *r = region_of(p->tree_blocks, who)) return r->part;
+  if (p->tree_blocks.size() >= size_t(kDecMaxRegions)) return nullptr;
+  try {
+    p->tree_blocks.reserve(p->tree_blocks.size() + 1);
+    p->ctx->tree_free.reserve(p->ctx->tree_free.size() + p->tree_blocks.size() + 1);    // what this plan will give back
+  } catch (const std::bad_alloc &) {
+    return nullptr;
+  }
+  void *block = nullptr;
+  if (!p->ctx->tree_free.empty()) {
+    block = p->ctx->tree_free.back();
+    p->ctx->tree_free.pop_back();
+  } else {                                              // perhaps under capture, see more_decode_regions
+    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+    if (hipThreadExchangeStreamCaptureMode(&mode) != hipSuccess) { (void)hipGetLastError(); return nullptr; }
+    if (hipMalloc(&block, kTreePartBytes) != hipSuccess) { (void)hipGetLastError(); block = nullptr; }
+    (void)hipThreadExchangeStreamCaptureMode(&mode);
+    if (!block) return nullptr;
+  }
+  p->tree_blocks.push_back({block, nullptr, who.stream, who.capture, who.thread, true});
+  return block;
 }
 
 namespace {
@@ -1062,6 +1099,8 @@ extern "C" sp_status sp_plan_update(sp_plan *plan, const sp_segtable *t) {
   } else {
     drop_decode_blocks(ctx, plan);
   }
+  fresh.tree_blocks = std::move(plan->tree_blocks);
+  for (sp::DecodeRegion &r : fresh.tree_blocks) r.taken = false;
   *plan = std::move(fresh);
   fresh.dev_blob = nullptr;
   return SP_OK;
@@ -1073,6 +1112,7 @@ extern "C" void sp_plan_destroy(sp_plan *plan) {
   if (plan->dev_blob) give_back_block(ctx, plan->dev_blob, plan->dev_blob_bytes);
   drop_decode_blocks(ctx, plan);
   if (plan->dec_scratch) ctx->dec_free.push_back({plan->dec_scratch, plan->dec_scratch_bytes});
+  for (const sp::DecodeRegion &r : plan->tree_blocks) ctx->tree_free.push_back(r.part);
   delete plan;
   if (ctx) ctx_unref(ctx);
 }
@@ -1381,10 +1421,12 @@ extern "C" sp_status sp_tree_decode(sp_ctx *ctx, const sp_plan *plan, const int3
   if (o_out == q_new || o_out == k_new || o_out == v_new)
     return fail(&ctx->err, SP_ERR_INVALID_ARG, "o_out must not alias an input");
   SP_HIP(ctx, hipSetDevice(ctx->device));
+  bool no_scratch = false;
   hipError_t e = sp::launch_tree_decode(
       plan, sp::TreeArgs{kept, k, K_prefill, V_prefill, kv_tok_stride, kv_head_stride, K_resp, V_resp, pos_resp, resp_capacity, resp_len,
                          resp_len_add, parent, n_nodes, max_nodes, new_pos, q_new, k_new, v_new, o_out, softmax_scale, 0},
-      ctx->stream);
+      ctx->stream, &no_scratch);
+  if (no_scratch) return fail(&ctx->err, SP_ERR_WORKSPACE, "no scratch for a tree decode on this stream or capture");
   if (e != hipSuccess) return fail(&ctx->err, SP_ERR_HIP, "tree decode launch: %s", hipGetErrorString(e));
   return SP_OK;
 }

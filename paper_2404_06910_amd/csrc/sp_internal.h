@@ -183,6 +183,7 @@ struct sp_ctx {
   char *dec_at = nullptr;
   size_t dec_left = 0;
   std::vector<std::pair<void *, size_t>> dec_free;
+  std::vector<void *> tree_free;            // scratch of the trees of plans that are gone, for the next ones
   int refs = 1;               // the context itself + every live plan made on it
   bool closed = false;        // sp_destroy was called; the struct lives on until the last plan is gone
 };
@@ -228,6 +229,9 @@ struct sp_plan {
   size_t dec_scratch_bytes = 0;
   mutable std::vector<sp::DecodeRegion> dec_regions;
   mutable std::vector<std::pair<void *, size_t>> dec_blocks;
+  // Scratch of tree launches that are cut into pieces: a block per order of execution too, from the context's or new, kept
+  // over updates and given back to the context with the plan.  It holds partial sums only, nothing that has to be zero before.
+  mutable std::vector<sp::DecodeRegion> tree_blocks;
   // device copies (one allocation)
   void *dev_blob = nullptr;
   size_t dev_blob_bytes = 0;  // capacity of the allocation
@@ -295,7 +299,12 @@ struct TreeArgs {
   float scale;
   int32_t few_wgs;                      // see build_key_table
 };
-hipError_t launch_tree_decode(const sp_plan *plan, TreeArgs a, hipStream_t s);
+// Partial sums of a launch whose key lists are cut into pieces: at most this much.
+constexpr size_t kTreePartBytes = size_t(16) << 20;
+// A block of that size for a launch on stream s, or nullptr when there is none to be had.
+void *tree_scratch(const sp_plan *plan, hipStream_t s);
+// *no_scratch: nothing was launched, because there was none.
+hipError_t launch_tree_decode(const sp_plan *plan, const TreeArgs &a, hipStream_t s, bool *no_scratch);
 
 struct SampleArgs {
   const void *logits;
