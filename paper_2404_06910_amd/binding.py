@@ -122,11 +122,15 @@ def _dev(t, what: str) -> int:
     return t.data_ptr()
 
 
-def _table_dev(t, what: str, dtype: str, n: Optional[int]):
+# These are called for every small table of every token and layer: one expression where all is well, and what was wrong is found
+# out only where something is.
+def _table_dev(t, what: str, dtype, n: Optional[int]):
     """Device pointer of a contiguous tensor of one 32-bit type (and size); None -> NULL."""
     if t is None:
         return None
-    if str(t.dtype) != dtype or not t.is_contiguous():
+    if t.dtype is dtype and t.is_cuda and t.is_contiguous() and (n is None or t.numel() == n):
+        return t.data_ptr()
+    if t.dtype is not dtype or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor" % (what, dtype))
     if n is not None and t.numel() != n:
         raise ValueError("%s has %d entries, expected %d" % (what, t.numel(), n))
@@ -134,18 +138,30 @@ def _table_dev(t, what: str, dtype: str, n: Optional[int]):
 
 
 def _i32_dev(t, what: str, n: Optional[int] = None):
-    return _table_dev(t, what, "torch.int32", n)
+    return None if t is None else _table_dev(t, what, _torch().int32, n)
 
 
 def _f32_dev(t, what: str, n: Optional[int] = None):
-    return _table_dev(t, what, "torch.float32", n)
+    return None if t is None else _table_dev(t, what, _torch().float32, n)
+
+
+_TORCH = None
+
+
+def _torch():
+    """torch, imported at its first use: host-only plans do without."""
+    global _TORCH
+    if _TORCH is None:
+        import torch
+        _TORCH = torch
+    return _TORCH
 
 
 def _dtype_code(t) -> int:
-    import torch
-    if t.dtype == torch.float32:
+    torch = _torch()
+    if t.dtype is torch.float32:
         return SP_F32
-    if t.dtype == torch.bfloat16:
+    if t.dtype is torch.bfloat16:
         return SP_BF16
     raise ValueError("unsupported tensor dtype %s" % t.dtype)
 
@@ -254,22 +270,36 @@ class Context:
         ks = K_prefill.stride()
         if ks != V_prefill.stride() or ks[-1] != 1:
             raise ValueError("K_prefill and V_prefill must share strides, inner stride 1")
-        B, N = q_new.shape[:2]
-        if q_new.dim() != 4 or B != plan.n_prompts or o_out.shape != q_new.shape:
+        shape, new = q_new.shape, k_new.shape
+        if len(shape) != 4 or shape[0] != plan.n_prompts or o_out.shape != shape:
             raise ValueError("q_new and o_out must be [n_prompts, max_nodes, n_q_heads, head_dim]")
-        if k_new.shape[:2] != (B, N) or v_new.shape != k_new.shape:
+        if len(new) != 4 or new[:2] != shape[:2] or v_new.shape != new:
             raise ValueError("k_new and v_new must be [n_prompts, max_nodes, n_kv_heads, head_dim]")
-        for t, n in ((K_resp, "K_resp"), (V_resp, "V_resp"), (q_new, "q_new"), (k_new, "k_new"), (v_new, "v_new"), (o_out, "o_out")):
-            if not t.is_contiguous():
-                raise ValueError("%s must be contiguous" % n)
-            if _dtype_code(t) != plan.dtype:
-                raise ValueError("%s does not have the plan's dtype" % n)
-        self._check(lib().sp_tree_decode(
-            self._h, plan._h, _i32_dev(kept, "kept"), int(k), _dev(K_prefill, "K_prefill"), _dev(V_prefill, "V_prefill"),
-            ks[0], ks[1], _dev(K_resp, "K_resp"), _dev(V_resp, "V_resp"), _f32_dev(pos_resp, "pos_resp"), int(resp_capacity),
+        B, N = shape[:2]
+        dt = _torch().float32 if plan.dtype == SP_F32 else _torch().bfloat16
+        if not (K_resp.is_contiguous() and V_resp.is_contiguous() and q_new.is_contiguous() and k_new.is_contiguous()
+                and v_new.is_contiguous() and o_out.is_contiguous() and K_prefill.is_cuda and V_prefill.is_cuda and K_resp.is_cuda
+                and V_resp.is_cuda and q_new.is_cuda and k_new.is_cuda and v_new.is_cuda and o_out.is_cuda
+                and K_prefill.dtype is dt and V_prefill.dtype is dt and K_resp.dtype is dt and V_resp.dtype is dt
+                and q_new.dtype is dt and k_new.dtype is dt and v_new.dtype is dt and o_out.dtype is dt):
+            named = ((K_resp, "K_resp"), (V_resp, "V_resp"), (q_new, "q_new"), (k_new, "k_new"), (v_new, "v_new"), (o_out, "o_out"))
+            for t, n in named:
+                if not t.is_contiguous():
+                    raise ValueError("%s must be contiguous" % n)
+            named += ((K_prefill, "K_prefill"), (V_prefill, "V_prefill"))
+            for t, n in named:
+                if t.dtype is not dt:
+                    raise ValueError("%s does not have the plan's dtype" % n)
+            for t, n in named:
+                _dev(t, n)
+        st = lib().sp_tree_decode(
+            self._h, plan._h, _i32_dev(kept, "kept"), int(k), K_prefill.data_ptr(), V_prefill.data_ptr(), ks[0], ks[1],
+            K_resp.data_ptr(), V_resp.data_ptr(), _f32_dev(pos_resp, "pos_resp"), int(resp_capacity),
             _i32_dev(resp_len, "resp_len", B), int(resp_len_add), _i32_dev(parent, "parent", B * N),
-            _i32_dev(n_nodes, "n_nodes", B), N, _f32_dev(new_pos, "new_pos", B * N), _dev(q_new, "q_new"), _dev(k_new, "k_new"),
-            _dev(v_new, "v_new"), _dev(o_out, "o_out"), float(softmax_scale)))
+            _i32_dev(n_nodes, "n_nodes", B), N, _f32_dev(new_pos, "new_pos", B * N), q_new.data_ptr(), k_new.data_ptr(),
+            v_new.data_ptr(), o_out.data_ptr(), float(softmax_scale))
+        if st != 0:
+            self._check(st)
         return o_out
 
     # -- a6 ------------------------------------------------------------------------------

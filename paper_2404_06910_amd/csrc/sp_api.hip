@@ -215,23 +215,29 @@ static sp_status ensure_sal(sp_ctx *ctx, int64_t n_rows, int32_t n_slots) {
   return SP_OK;
 }
 
-// Further decode regions for a plan, as many as it has.  This may happen while a stream is being captured: the allocation
-// and the zeroing (on a stream of its own, waited for) are no part of the capture, and the calls are made in the mode that
-// lets them be.
-static bool more_decode_regions(const sp_plan *p) {
-  const size_t have = p->dec_regions.size(), n = std::min(have, sp::kDecMaxRegions - have);
-  if (n == 0) return false;
+// Device memory of which a part is zero.  This may happen while a stream is being captured: the allocation and the zeroing (on a
+// stream of its own, waited for) are no part of the capture, and the calls are made in the mode that lets them be.
+static void *zeroed_block(size_t bytes, size_t zero_at, size_t zero_bytes) {
   hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
-  if (hipThreadExchangeStreamCaptureMode(&mode) != hipSuccess) return false;
-  const size_t bytes = n * (p->dec_count_bytes + p->dec_part_bytes);
+  if (hipThreadExchangeStreamCaptureMode(&mode) != hipSuccess) return nullptr;
   void *block = nullptr;
   hipStream_t own = nullptr;
-  bool ok = hipMalloc(&block, bytes) == hipSuccess && hipStreamCreateWithFlags(&own, hipStreamNonBlocking) == hipSuccess &&
-            hipMemsetAsync(block, 0, n * p->dec_count_bytes, own) == hipSuccess && hipStreamSynchronize(own) == hipSuccess;
+  const bool ok = hipMalloc(&block, bytes) == hipSuccess && hipStreamCreateWithFlags(&own, hipStreamNonBlocking) == hipSuccess &&
+                  hipMemsetAsync(static_cast<char *>(block) + zero_at, 0, zero_bytes, own) == hipSuccess &&
+                  hipStreamSynchronize(own) == hipSuccess;
   if (own) (void)hipStreamDestroy(own);
   if (!ok && block) (void)hipFree(block);
   (void)hipThreadExchangeStreamCaptureMode(&mode);
-  if (!ok) return false;
+  return ok ? block : nullptr;
+}
+
+// Further decode regions for a plan, as many as it has.
+static bool more_decode_regions(const sp_plan *p) {
+  const size_t have = p->dec_regions.size(), n = std::min(have, sp::kDecMaxRegions - have);
+  if (n == 0) return false;
+  const size_t bytes = n * (p->dec_count_bytes + p->dec_part_bytes);
+  void *block = zeroed_block(bytes, 0, n * p->dec_count_bytes);
+  if (!block) return false;
   p->dec_blocks.push_back({block, bytes});
   for (size_t i = 0; i < n; ++i)
     p->dec_regions.push_back({static_cast<char *>(block) + n * p->dec_count_bytes + i * p->dec_part_bytes,
@@ -287,10 +293,10 @@ const sp::DecodeRegion *sp::decode_region(const sp_plan *p, hipStream_t s) {
   return region_of(p->dec_regions, who);
 }
 
-void *sp::tree_scratch(const sp_plan *p, hipStream_t s) {
+const sp::DecodeRegion *sp::tree_region(const sp_plan *p, hipStream_t s) {
   DecodeRegion who{};
   if (!execution_order(s, &who)) return nullptr;
-  if (DecodeRegion *r = region_of(p->tree_blocks, who)) return r->part;
+  if (const DecodeRegion *r = region_of(p->tree_blocks, who)) return r;
   if (p->tree_blocks.size() >= size_t(kDecMaxRegions)) return nullptr;
   try {
     p->tree_blocks.reserve(p->tree_blocks.size() + 1);
@@ -302,15 +308,13 @@ void *sp::tree_scratch(const sp_plan *p, hipStream_t s) {
   if (!p->ctx->tree_free.empty()) {
     block = p->ctx->tree_free.back();
     p->ctx->tree_free.pop_back();
-  } else {                                              // perhaps under capture, see more_decode_regions
-    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
-    if (hipThreadExchangeStreamCaptureMode(&mode) != hipSuccess) { (void)hipGetLastError(); return nullptr; }
-    if (hipMalloc(&block, kTreePartBytes) != hipSuccess) { (void)hipGetLastError(); block = nullptr; }
-    (void)hipThreadExchangeStreamCaptureMode(&mode);
-    if (!block) return nullptr;
+  } else if (!(block = zeroed_block(kTreePartBytes + kTreeCounters * sizeof(uint32_t), kTreePartBytes, kTreeCounters * sizeof(uint32_t)))) {
+    (void)hipGetLastError();
+    return nullptr;
   }
-  p->tree_blocks.push_back({block, nullptr, who.stream, who.capture, who.thread, true});
-  return block;
+  p->tree_blocks.push_back({block, reinterpret_cast<uint32_t *>(static_cast<char *>(block) + kTreePartBytes), who.stream, who.capture,
+                            who.thread, true});
+  return &p->tree_blocks.back();
 }
 
 namespace {

@@ -230,7 +230,7 @@ struct sp_plan {
   mutable std::vector<sp::DecodeRegion> dec_regions;
   mutable std::vector<std::pair<void *, size_t>> dec_blocks;
   // Scratch of tree launches that are cut into pieces: a block per order of execution too, from the context's or new, kept
-  // over updates and given back to the context with the plan.  It holds partial sums only, nothing that has to be zero before.
+  // over updates and given back to the context with the plan (counters behind the partial sums; every launch leaves them zero).
   mutable std::vector<sp::DecodeRegion> tree_blocks;
   // device copies (one allocation)
   void *dev_blob = nullptr;
@@ -299,10 +299,11 @@ struct TreeArgs {
   float scale;
   int32_t few_wgs;                      // see build_key_table
 };
-// Partial sums of a launch whose key lists are cut into pieces: at most this much.
+// What a launch whose key lists are cut into pieces has at most: partial sums, and arrival counters (zero between launches).
 constexpr size_t kTreePartBytes = size_t(16) << 20;
-// A block of that size for a launch on stream s, or nullptr when there is none to be had.
-void *tree_scratch(const sp_plan *plan, hipStream_t s);
+constexpr int kTreeCounters = 2048;
+// A region of that size for a launch on stream s, or nullptr when there is none to be had.
+const DecodeRegion *tree_region(const sp_plan *plan, hipStream_t s);
 // *no_scratch: nothing was launched, because there was none.
 hipError_t launch_tree_decode(const sp_plan *plan, const TreeArgs &a, hipStream_t s, bool *no_scratch);
 

@@ -27,7 +27,14 @@ __device__ __forceinline__ void dma16(const void *gptr, uint32_t lds_base) {
 
 // The same with the address split into a wave-uniform base (scalar registers) and a 32-bit per-lane
 // byte offset: no vector arithmetic per instruction and no 64-bit per-lane pointers to keep alive.
+// NT: for rows that nobody else reads.
+template <bool NT = false>
 __device__ __forceinline__ void dma16s(const void *sbase, uint32_t voff, uint32_t lds_base) {
+  if constexpr (NT) {
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(lds_base), "v"(voff), "s"(sbase)
+                 : "memory", "m0");
+    return;
+  }
   asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_base), "v"(voff), "s"(sbase)
                : "memory", "m0");
 }

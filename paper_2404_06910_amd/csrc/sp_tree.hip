@@ -7,8 +7,8 @@
 // A wave walks the keys 32 (fp32: 16) at a time for RT tiles of 16 rows, with a running maximum and sum per row.  The waves of a
 // workgroup either take different keys (few rows: nothing is shared, each wave streams through two LDS slots of its own and waits for
 // nobody, their sums are added up at the end) or different rows (many rows: K and V are staged once for all of them).
-// Where that leaves most of the chip idle, the key list is cut into pieces too, one workgroup each, and a
-// second, small kernel adds the pieces up in their order.
+// Where that leaves most of the chip idle, the key list is cut into pieces too, one workgroup each, and the workgroup that
+// finishes last adds the pieces up in their order.
 #include <algorithm>
 #include <type_traits>
 
@@ -19,24 +19,27 @@ namespace sp {
 
 namespace {
 
+typedef __attribute__((ext_vector_type(2))) unsigned long long u64x2;
+
 struct TreeDev {
   TreeArgs a;
   int32_t n_pieces;
   float *part;               // n_pieces > 1: [piece][prompt, node, query head][D] sums, then {max, sum} for each
   int64_t rows;              // prompts * nodes * query heads
+  uint32_t *count;           // and an arrival counter per (prompt, KV head, block of rows), zero between launches
 };
 
-// Bit j of lane i's mask: node j is node i or an ancestor of it.  Six doublings reach all of 64 nodes, since parents come first.
-__device__ __forceinline__ uint64_t ancestor_mask(const int32_t *parent, int64_t base, int n) {
+// The parent of lane i's node as the table has it (the request leaves early, the mask is built when K and V are on their way).
+__device__ __forceinline__ int load_parent(const TreeArgs &a, int b) {
   const int i = threadIdx.x & 63;
-  int up = -1;
-  if (i < n) {
-    up = parent ? parent[base + i] : i - 1;
-    if (up < 0 || up >= i) up = -1;
-  }
+  return a.parent && i < a.max_nodes ? a.parent[(int64_t)b * a.max_nodes + i] : i - 1;
+}
+// Bit j of lane i's mask: node j is node i or an ancestor of it.  Six doublings reach all of 64 nodes, since parents come first.
+__device__ __forceinline__ uint64_t ancestor_mask(int up, int n) {
+  const int i = threadIdx.x & 63;
+  if (i >= n || up < 0 || up >= i) up = -1;
   uint32_t lo = i < 32 ? 1u << i : 0u, hi = i >= 32 ? 1u << (i - 32) : 0u;
-#pragma unroll
-  for (int r = 0; r < 6; ++r) {
+  for (int r = 1; r < n; r *= 2) {
     const int from = up < 0 ? i : up;
     const uint32_t l = __shfl(lo, from), h = __shfl(hi, from);
     const int u = __shfl(up, from);
@@ -47,7 +50,7 @@ __device__ __forceinline__ uint64_t ancestor_mask(const int32_t *parent, int64_t
   return uint64_t(hi) << 32 | lo;
 }
 
-// the nodes' K and V (and positions) to the response cache: one workgroup per (prompt, KV head)
+// the nodes' K and V (and positions) to the response cache: workgroups of their own, one per (prompt, KV head), beside the others
 template <typename T, int D>
 __device__ __forceinline__ void append_nodes(const PlanDev &pd, const TreeArgs &a, int b, int g, int row0, int n) {
   constexpr int EV = Elem<T>::kVec, LPK = D / EV;
@@ -78,30 +81,34 @@ __device__ __forceinline__ float rows_sum(float x) {
 // What a wave needs to know of its rows: lane L holds row L % 16 of each tile.
 template <int RT>
 struct Rows {
-  int32_t node[RT], head[RT];        // rows past the last repeat it
+  int32_t node[RT], head[RT];        // rows past max_nodes repeat the last one
   bool real[RT];
   uint64_t mask[RT];                 // nodes that the row sees
   float slope2[RT], bias0[RT];       // with a distance penalty: slope * log2 e, and that times minus the row's position
 };
 template <int RT, bool BIAS>
-__device__ __forceinline__ void find_rows(const PlanDev &pd, const TreeArgs &a, int b, int g, int n, int row0, Rows<RT> &r) {
+__device__ __forceinline__ void find_rows(const PlanDev &pd, const TreeArgs &a, int b, int g, int row0, Rows<RT> &r) {
   const int G = pd.n_q_heads / pd.n_kv_heads, l16 = threadIdx.x & 15;
-  const uint64_t all = ancestor_mask(a.parent, (int64_t)b * a.max_nodes, n);
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    const int row = min(row0 + 16 * t + l16, n * G - 1);
-    r.real[t] = row0 + 16 * t + l16 < n * G;
+    const int row = min(row0 + 16 * t + l16, a.max_nodes * G - 1);
     r.node[t] = row / G;
     r.head[t] = g * G + row % G;
-    r.mask[t] = uint64_t(__shfl(uint32_t(all >> 32), r.node[t])) << 32 | __shfl(uint32_t(all), r.node[t]);
     r.slope2[t] = BIAS ? pd.slopes[r.head[t]] * kLog2e : 0.f;
     r.bias0[t] = BIAS ? -r.slope2[t] * a.new_pos[(int64_t)b * a.max_nodes + r.node[t]] : 0.f;
   }
 }
+template <int RT>
+__device__ __forceinline__ void find_masks(const PlanDev &pd, int n, int up, int row0, Rows<RT> &r) {
+  const int G = pd.n_q_heads / pd.n_kv_heads, l16 = threadIdx.x & 15;
+  const uint64_t all = ancestor_mask(up, n);
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    r.real[t] = row0 + 16 * t + l16 < n * G;
+    r.mask[t] = uint64_t(__shfl(uint32_t(all >> 32), r.node[t])) << 32 | __shfl(uint32_t(all), r.node[t]);
+  }
+}
 
-// Ends a workgroup.  Every wave has m, l (complete, the same in a row's four lanes) and the weighted sums of its rows; Put says
-// which dims a lane holds: put(t, fn) calls fn(first dim, four sums) for each of its groups of four.  Waves that took different keys
-// (KEYS of them) are added up in LDS, in their order.
 template <typename T, int D>
 __device__ __forceinline__ void store4(const TreeDev &d, int64_t row, int dim, f32x4 v, float inv) {
   if constexpr (sizeof(T) == 2) {
@@ -113,62 +120,121 @@ __device__ __forceinline__ void store4(const TreeDev &d, int64_t row, int dim, f
     *reinterpret_cast<f32x4 *>(static_cast<float *>(d.a.o_out) + row * D + dim) = v * inv;
   }
 }
-template <typename T, int D, int RT, int KEYS, class Put>
-__device__ __forceinline__ void finish(const PlanDev &pd, const TreeDev &d, int b, const Rows<RT> &r, const float *m, const float *l,
-                                       float *lds, Put &&put) {
-  constexpr int PITCH = D + 4;                       // 16 rows' vectors fall into different banks
-  const int lane = threadIdx.x & 63, l16 = lane & 15, wave = threadIdx.x >> 6;
-  const int64_t base = (int64_t)b * d.a.max_nodes * pd.n_q_heads;
-  auto out = [&](int64_t row, int dim, f32x4 v, float mm, float ll, bool first) {
-    if (d.n_pieces == 1) {
-      store4<T, D>(d, row, dim, v, 1.f / ll);
-    } else {
-      const int64_t at = int64_t(blockIdx.z) * d.rows + row;
-      *reinterpret_cast<f32x4 *>(d.part + at * D + dim) = v;
-      if (first) {
-        d.part[d.n_pieces * d.rows * D + 2 * at] = mm;
-        d.part[d.n_pieces * d.rows * D + 2 * at + 1] = ll;
-      }
-    }
-  };
-  if constexpr (KEYS == 1) {
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      const int64_t row = base + (int64_t)r.node[t] * pd.n_q_heads + r.head[t];
-      put(t, [&](int dim, f32x4 v) {
-        if (r.real[t]) out(row, dim, v, m[t], l[t], dim == 0);
-      });
-    }
-  } else {
-    __shared__ float s_m[KEYS][16 * RT], s_l[KEYS][16 * RT];
+
+// Four floats that other workgroups write or read: agent-scope accesses go past the L2 that is not theirs (a fence would write
+// back and invalidate all of it).
+__device__ __forceinline__ void store_shared(float *p, f32x4 v) {
+  const auto w = __builtin_bit_cast(u64x2, v);
+  __hip_atomic_store(reinterpret_cast<unsigned long long *>(p), w[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store(reinterpret_cast<unsigned long long *>(p) + 1, w[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x4 load_shared(const float *p) {
+  u64x2 w;
+  w[0] = __hip_atomic_load(reinterpret_cast<const unsigned long long *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  w[1] = __hip_atomic_load(reinterpret_cast<const unsigned long long *>(p) + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return __builtin_bit_cast(f32x4, w);
+}
+
+// Ends a workgroup.  Every wave has m, l (complete, the same in a row's four lanes) and the weighted sums of its rows, NV vectors of
+// four dims of which the i-th begins at dim(i).  The KS groups of waves that took different keys are added up in LDS, in their order, by the
+// first group; pieces, if there are several, by the workgroup that arrives last, in theirs.
+template <typename T, int D, int RT, int RW, int KS, class Dim>
+__device__ __forceinline__ void finish(const PlanDev &pd, const TreeDev &d, int b, int g, int n, const Rows<RT> &r, float *m, float *l,
+                                       f32x4 (*o)[D / 16], float *lds, Dim &&dim) {
+  constexpr int PITCH = D + 4, NV = D / 16;          // 16 rows' vectors fall into different banks
+  const int lane = threadIdx.x & 63, l16 = lane & 15, wave = threadIdx.x >> 6, rw = wave % RW, ks = wave / RW;
+  if constexpr (KS > 1) {
+    __shared__ float s_ml[KS - 1][RW][2][16 * RT];
     __syncthreads();                                 // all waves are done with their slots
+    if (ks > 0) {
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      put(t, [&](int dim, f32x4 v) { *reinterpret_cast<f32x4 *>(lds + ((wave * RT + t) * 16 + l16) * PITCH + dim) = v; });
-      if (lane < 16) { s_m[wave][16 * t + lane] = m[t]; s_l[wave][16 * t + lane] = l[t]; }
+      for (int t = 0; t < RT; ++t) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+          *reinterpret_cast<f32x4 *>(lds + ((((ks - 1) * RW + rw) * RT + t) * 16 + l16) * PITCH + dim(i)) = o[t][i];
+        if (lane < 16) { s_ml[ks - 1][rw][0][16 * t + lane] = m[t]; s_ml[ks - 1][rw][1][16 * t + lane] = l[t]; }
+      }
     }
     __syncthreads();
-    constexpr int PER = D / 4;
-    const int G = pd.n_q_heads / pd.n_kv_heads;
-    for (int i = threadIdx.x; i < 16 * RT * PER; i += 64 * KEYS) {
-      const int at = i / PER, dim = i % PER * 4;
-      float mm = s_m[0][at], ll = 0.f;
-      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (ks == 0) {
 #pragma unroll
-      for (int w = 1; w < KEYS; ++w) mm = fmaxf(mm, s_m[w][at]);
+      for (int t = 0; t < RT; ++t)
 #pragma unroll
-      for (int w = 0; w < KEYS; ++w) {
-        const float f = fast_exp2(s_m[w][at] - mm);
-        const f32x4 x = *reinterpret_cast<const f32x4 *>(lds + (w * 16 * RT + at) * PITCH + dim);
-        ll = fmaf(f, s_l[w][at], ll);
+        for (int k = 0; k < KS - 1; ++k) {
+          const float pm = s_ml[k][rw][0][16 * t + l16], m_new = fmaxf(m[t], pm), wa = fast_exp2(m[t] - m_new), wb = fast_exp2(pm - m_new);
+          l[t] = l[t] * wa + s_ml[k][rw][1][16 * t + l16] * wb;
+          m[t] = m_new;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = fmaf(f, x[e], v[e]);
-      }
-      // the row itself: that of tile at / 16, lane at % 16
-      const int first = int(blockIdx.y) * 16 * RT, rr = first + at;
-      const int n = d.a.n_nodes ? min(max(d.a.n_nodes[b], 0), d.a.max_nodes) : d.a.max_nodes;
-      if (rr < n * G) out(base + int64_t(rr / G) * pd.n_q_heads + int64_t(blockIdx.x % pd.n_kv_heads) * G + rr % G, dim, v, mm, ll, dim == 0);
+          for (int i = 0; i < NV; ++i) {
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(lds + (((k * RW + rw) * RT + t) * 16 + l16) * PITCH + dim(i));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[t][i][e] = o[t][i][e] * wa + x[e] * wb;
+          }
+        }
     }
+  }
+  const int64_t base = (int64_t)b * d.a.max_nodes * pd.n_q_heads;
+  float *const part_ml = d.part + d.n_pieces * d.rows * D;
+  if (ks == 0) {
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      if (!r.real[t]) continue;
+      const int64_t row = base + (int64_t)r.node[t] * pd.n_q_heads + r.head[t];
+      if (d.n_pieces == 1) {
+        const float inv = 1.f / l[t];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) store4<T, D>(d, row, dim(i), o[t][i], inv);
+      } else {
+        const int64_t at = int64_t(blockIdx.z) * d.rows + row;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) store_shared(d.part + at * D + dim(i), o[t][i]);
+        if (lane < 16) {
+          const uint64_t w = uint64_t(__float_as_uint(l[t])) << 32 | __float_as_uint(m[t]);
+          __hip_atomic_store(reinterpret_cast<unsigned long long *>(part_ml + 2 * at), w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+      }
+    }
+  }
+  if (d.n_pieces == 1) return;
+  __shared__ int s_last;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's stores have been performed
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    uint32_t *ctr = d.count + blockIdx.x + gridDim.x * blockIdx.y;
+    s_last = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == uint32_t(d.n_pieces - 1);
+    if (s_last) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  if (!s_last) return;
+  // a thread per row and four dims
+  constexpr int PER = D / 4;
+  const int G = pd.n_q_heads / pd.n_kv_heads, row0 = int(blockIdx.y) * RW * RT * 16, rows = min(RW * RT * 16, n * G - row0);
+  for (int i = threadIdx.x; i < rows * PER; i += 64 * RW * KS) {
+    const int rr = row0 + i / PER, at_dim = i % PER * 4;
+    const int64_t row = base + int64_t(rr / G) * pd.n_q_heads + g * G + rr % G;
+    float mm = kNegBig, ll = 0.f;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    for (int p0 = 0; p0 < d.n_pieces; p0 += 4) {     // four pieces' loads in flight
+      f32x4 x[4];
+      uint64_t w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int64_t at = min(p0 + j, d.n_pieces - 1) * d.rows + row;
+        x[j] = load_shared(d.part + at * D + at_dim);
+        w[j] = __hip_atomic_load(reinterpret_cast<unsigned long long *>(part_ml + 2 * at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (p0 + j >= d.n_pieces) break;
+        const float pm = __uint_as_float(uint32_t(w[j])), pl = __uint_as_float(uint32_t(w[j] >> 32));
+        const float m_new = fmaxf(mm, pm), wa = fast_exp2(mm - m_new), wb = fast_exp2(pm - m_new);
+        ll = ll * wa + pl * wb;
+        mm = m_new;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = v[e] * wa + x[j][e] * wb;
+      }
+    }
+    store4<T, D>(d, row, at_dim, v, 1.f / ll);
   }
 }
 
@@ -182,29 +248,35 @@ __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x)
 // In the accumulator lane L holds row L % 16 and keys 4 (L / 16) + i of each tile, which are bound to the k-slots that the lane feeds in
 // the second product.  P is rounded to bf16 there, as the output is (the sum of the weights is not); that is half a step of every weight, and the
 // result is as far off as two roundings of it instead of one.
-// SHARED: the NW waves take different rows and fill each stage together; otherwise each takes every NW-th step and fills its own.
-template <int D, int RT, int NW, bool SHARED, bool BIAS>
-__global__ __launch_bounds__(64 * NW) void tree_bf16_kernel(PlanDev pd, TreeDev d) {
+// RW waves take different rows and fill each stage together; KS such groups take every KS-th step and have slots of their own.
+template <int D, int RT, int RW, int KS, int NS, bool BIAS>
+__global__ __launch_bounds__(64 * RW * KS, 2) void tree_bf16_kernel(PlanDev pd, TreeDev d) {
   constexpr int ROWB = D * 2, CPR = D / 8, RPC = 256 / ROWB, RG = 64 / CPR;   // LDS row, its 16-byte chunks, rows per 256 bytes, rows per DMA
   constexpr int HALFB = 32 * ROWB, SLOTB = 2 * HALFB;
   constexpr int NI = 32 / RG;                    // DMA instructions per half
-  constexpr int KEYS = SHARED ? 1 : NW;
-  constexpr int RINGB = 2 * SLOTB * KEYS;
-  constexpr int MERGEB = KEYS > 1 ? KEYS * RT * 16 * (D + 4) * 4 : 0;
+  constexpr bool STREAM = RW == 1;               // one block of rows: nobody else reads these keys
+  constexpr int RINGB = NS * SLOTB * KS;
+  constexpr int MERGEB = (KS - 1) * RW * RT * 16 * (D + 4) * 4;
   constexpr int NJ = D / 32, NC = D / 16;
   __shared__ __attribute__((aligned(1024))) unsigned char ring[RINGB > MERGEB ? RINGB : MERGEB];
-  __shared__ __attribute__((aligned(256))) float s_pos[BIAS ? 2 * KEYS : 1][64];
+  __shared__ __attribute__((aligned(256))) float s_pos[BIAS ? NS * KS : 1][64];
   __shared__ KeyTable tab;
   const TreeArgs &a = d.a;
   const int Hq = pd.n_q_heads, Hkv = pd.n_kv_heads, G = Hq / Hkv;
   const int b = blockIdx.x / Hkv, g = blockIdx.x % Hkv;
   const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rw = wave % RW, ks = wave / RW;
+  const RespRows rr = resp_rows(a, b);
   const int n = a.n_nodes ? min(max(a.n_nodes[b], 0), a.max_nodes) : a.max_nodes;
-  const int row0 = (int(blockIdx.y) * (SHARED ? NW : 1) + (SHARED ? wave : 0)) * 16 * RT;
-  if (int(blockIdx.y) * (SHARED ? NW : 1) * 16 * RT >= n * G) return;
+  if (blockIdx.y == gridDim.y - 1) {
+    if (blockIdx.z == 0) append_nodes<__bf16, D>(pd, a, b, g, rr.write, n);
+    return;
+  }
+  const int row0 = (int(blockIdx.y) * RW + rw) * 16 * RT;
 
   Rows<RT> rows;
-  find_rows<RT, BIAS>(pd, a, b, g, n, row0, rows);
+  find_rows<RT, BIAS>(pd, a, b, g, row0, rows);
+  const int up = load_parent(a, b);
   bf16x8 qf[RT][NJ];
 #pragma unroll
   for (int t = 0; t < RT; ++t)
@@ -213,10 +285,16 @@ __global__ __launch_bounds__(64 * NW) void tree_bf16_kernel(PlanDev pd, TreeDev 
       qf[t][j] = *reinterpret_cast<const bf16x8 *>(static_cast<const __bf16 *>(a.q_new) +
                                                    (((int64_t)b * a.max_nodes + rows.node[t]) * Hq + rows.head[t]) * D + (q + 4 * j) * 8);
   const float scale2 = a.scale * kLog2e;
-  const RespRows rr = resp_rows(a, b);
-  if (blockIdx.y == 0 && blockIdx.z == 0) append_nodes<__bf16, D>(pd, a, b, g, rr.write, n);
+  if (int(blockIdx.y) * RW * 16 * RT >= n * G) return;
   build_key_table<__bf16, D>(pd, a, b, g, rr.read, NewKeys{b * a.max_nodes, n, int64_t(Hkv) * D * 2}, BIAS, tab);
   const RangeSearch find(tab);
+  // The compiler waits for a load of its own at the first use, which would be in the loop, with all the DMA in flight there.
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(qf[t][j]));
+  int up_here = up;
+  asm volatile("" : "+v"(up_here));
   const int n_total = tab.n_total, old = n_total - n;
   // pieces are multiples of 32 keys, so that only steps at the end of the list reach beyond it
   const int piece = ((n_total + d.n_pieces - 1) / d.n_pieces + 31) & ~31;
@@ -227,11 +305,12 @@ __global__ __launch_bounds__(64 * NW) void tree_bf16_kernel(PlanDev pd, TreeDev 
   // chunk) and transpose reads of V (8 rows of one chunk pair at a time) spread over the banks.
   auto fK = [](int row) { return (row / RPC) % CPR; };
   auto fV = [](int row) { return ((row / RPC) % (CPR / 4)) * 4 | ((row >> 2) & 1) * 2; };
-  const uint32_t ring_base = (uint32_t)(size_t)(lds_byte *)ring + (SHARED ? 0 : wave * 2 * SLOTB);
-  const uint32_t pos_base = (uint32_t)(size_t)(lds_byte *)&s_pos[0][0] + (SHARED ? 0 : wave * 2 * 256);
-  const unsigned char *ringp = ring + (SHARED ? 0 : wave * 2 * SLOTB);
+  const uint32_t ring_base = (uint32_t)(size_t)(lds_byte *)ring + ks * NS * SLOTB;
+  const uint32_t pos_base = (uint32_t)(size_t)(lds_byte *)&s_pos[0][0] + ks * NS * 256;
+  const unsigned char *ringp = ring + ks * NS * SLOTB;
   const int drow = lane / CPR, dslot = lane % CPR;
-  constexpr int MINE = SHARED ? (2 * NI + NW - 1) / NW : 2 * NI;           // DMA instructions of a wave per stage
+  static_assert(2 * NI % RW == 0, "the waves of a group share a stage evenly");
+  constexpr int MINE = 2 * NI / RW;              // DMA instructions of a wave per stage
 
   auto issue = [&](int s, int slot) {
     const int t0 = key0 + 32 * s;
@@ -244,22 +323,27 @@ __global__ __launch_bounds__(64 * NW) void tree_bf16_kernel(PlanDev pd, TreeDev 
     const char *kb = reinterpret_cast<const char *>(uniform64(reinterpret_cast<int64_t>(tab.k[i0]))) + (t0 - c0) * stride;
     const char *vb = reinterpret_cast<const char *>(uniform64(reinterpret_cast<int64_t>(tab.v[i0]))) + (t0 - c0) * stride;
     const uint32_t row_off = uint32_t(drow) * uint32_t(stride);
+    if (plain) {
 #pragma unroll
-    for (int x = 0; x < MINE; ++x) {
-      const int m2 = SHARED ? wave + x * NW : x;
-      if (SHARED && 2 * NI % NW != 0 && m2 >= 2 * NI) break;
-      const bool is_v = m2 >= NI;
-      const int m = is_v ? m2 - NI : m2, row = RG * m + drow;
-      const uint32_t chunk = uint32_t(dslot ^ (is_v ? fV(row) : fK(row))) * 16;
-      const uint32_t to = lds + (is_v ? HALFB : 0) + m * (RG * ROWB);
-      if (plain) {
-        dma16s((is_v ? vb : kb) + RG * m * stride, row_off + chunk, to);
-      } else {
+      for (int x = 0; x < MINE; ++x) {
+        const int m2 = rw + x * RW;
+        const bool is_v = m2 >= NI;
+        const int m = is_v ? m2 - NI : m2, row = RG * m + drow;
+        const uint32_t chunk = uint32_t(dslot ^ (is_v ? fV(row) : fK(row))) * 16;
+        dma16s<STREAM>((is_v ? vb : kb) + RG * m * stride, row_off + chunk, lds + (is_v ? HALFB : 0) + m * (RG * ROWB));
+      }
+    } else {
+#pragma unroll
+      for (int x = 0; x < MINE; ++x) {
+        const int m2 = rw + x * RW;
+        const bool is_v = m2 >= NI;
+        const int m = is_v ? m2 - NI : m2, row = RG * m + drow;
+        const uint32_t chunk = uint32_t(dslot ^ (is_v ? fV(row) : fK(row))) * 16;
         const int vk = min(t0 + row, n_total - 1), i = find.from(i0, vk);
-        dma16((is_v ? tab.v[i] : tab.k[i]) + int64_t(vk - tab.cum[i]) * tab.stride[i] + chunk, to);
+        dma16((is_v ? tab.v[i] : tab.k[i]) + int64_t(vk - tab.cum[i]) * tab.stride[i] + chunk, lds + (is_v ? HALFB : 0) + m * (RG * ROWB));
       }
     }
-    if (BIAS && (!SHARED || wave == 0)) {
+    if (BIAS && rw == 0) {
       const int vk = min(t0 + (lane & 31), n_total - 1), i = find.from(i0, vk);
       dma4(tab.pos[i] + (vk - tab.cum[i]), pos_base + slot * 256);
     }
@@ -276,65 +360,25 @@ __global__ __launch_bounds__(64 * NW) void tree_bf16_kernel(PlanDev pd, TreeDev 
   }
   const int tr_row = l16 >> 2, tr_x = (lane & 3) >> 1, tr_sub8 = (lane & 1) * 8;
 
-  // one step on a slot; MASKED: it holds nodes (or reaches beyond them)
-  auto step = [&](int t0, int slot, auto masked) {
-    constexpr bool MASKED = decltype(masked)::value;
+  // one step on a slot
+  auto compute = [&](int step, int slot) {
+    const int t0 = key0 + 32 * step;
+    const bool masked = t0 + 32 > old;               // it holds nodes, or reaches beyond them
     const unsigned char *sl = ringp + slot * SLOTB;
     f32x4 s[RT][2];
 #pragma unroll
     for (int t = 0; t < RT; ++t) s[t][0] = s[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) {
+      for (int h = 0; h < 2; ++h) {
         const int row = 16 * h + l16;
         const bf16x8 k = *reinterpret_cast<const bf16x8 *>(sl + row * ROWB + ((4 * j + q) ^ fK(row)) * 16);
 #pragma unroll
         for (int t = 0; t < RT; ++t) s[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[t][j], s[t][h], 0, 0, 0);
       }
-    f32x4 kp[2];
-    if (BIAS) {
-      const float *ps = &s_pos[(SHARED ? 0 : 2 * wave) + slot][0];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) kp[h] = *reinterpret_cast<const f32x4 *>(ps + 16 * h + 4 * q);
-    }
-    bf16x8 pb[RT];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      float mx = -INFINITY;
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float x = BIAS ? fmaf(s[t][h][i], scale2, fmaf(rows.slope2[t], kp[h][i], rows.bias0[t])) : s[t][h][i] * scale2;
-          if (MASKED) {
-            const int at = t0 + 16 * h + 4 * q + i - old;          // node of this key
-            if (at >= n || (at >= 0 && !(rows.mask[t] >> (at & 63) & 1))) x = -INFINITY;
-          }
-          s[t][h][i] = x;
-          mx = fmaxf(mx, x);
-        }
-      // The reference may lag behind the maximum by 8 (weights up to 256, which bf16 and the sums absorb): the lanes of a row need
-      // not agree on a maximum in every step.
-      if (__any(mx > m_run[t] + 8.f)) {
-        const float m_new = fmaxf(m_run[t], rows_max(mx)), alpha = fast_exp2(m_run[t] - m_new);
-        m_run[t] = m_new;
-        l_run[t] *= alpha;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) o[t][c] *= alpha;
-      }
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float p = fast_exp2(s[t][h][i] - m_run[t]);
-          l_run[t] += p;
-          pb[t][4 * h + i] = static_cast<__bf16>(p);
-        }
-    }
-    bf16x8 vf[NC];
+    bf16x8 vf[NC];                                   // on its way under the softmax
     const unsigned char *vs = sl + HALFB + tr_sub8;
-    uint32_t bad = 0;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       const int r0 = 4 * q + tr_row;
@@ -342,107 +386,167 @@ __global__ __launch_bounds__(64 * NW) void tree_bf16_kernel(PlanDev pd, TreeDev 
       const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)vp);
       const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(vp + 16 * ROWB));
       vf[c] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      if (MASKED) {
+    }
+    if (BIAS) {
+      const float *ps = &s_pos[NS * ks + slot][0];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const f32x4 kp = *reinterpret_cast<const f32x4 *>(ps + 16 * h + 4 * q);
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[t][h][i] = fmaf(s[t][h][i], scale2, fmaf(rows.slope2[t], kp[i], rows.bias0[t]));
+      }
+    }
+    auto largest = [](const f32x4 (&x)[2]) {
+      return fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
+    };
+    float mx[RT];
+    if (!masked) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) mx[t] = largest(s[t]);
+    } else {
+      // bit k of `see`: the row sees key t0 + k (all keys before the nodes)
+      const int at = t0 - old;
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        const uint32_t see = (at >= 0 ? uint32_t(rows.mask[t] >> at) : uint32_t(rows.mask[t]) << -at | ((1u << -at) - 1)) >> (4 * q);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[t][h][i] = see >> (16 * h + i) & 1 ? s[t][h][i] : -INFINITY;
+        mx[t] = largest(s[t]);
+      }
+    }
+    u32x4 pb[RT];                                    // weights as pairs of bf16
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      if (!BIAS) mx[t] *= scale2;                    // scale2 > 0
+      // The reference may lag behind the maximum by 8 (weights up to 256, which bf16 and the sums absorb): the lanes of a row need
+      // not agree on a maximum in every step.
+      if (__any(mx[t] > m_run[t] + 8.f)) {
+        const float m_new = fmaxf(m_run[t], rows_max(mx[t])), alpha = fast_exp2(m_run[t] - m_new);
+        m_run[t] = m_new;
+        l_run[t] *= alpha;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) o[t][c] *= alpha;
+      }
+      float ls[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = fast_exp2(BIAS ? s[t][h][i] - m_run[t] : fmaf(s[t][h][i], scale2, -m_run[t]));
+        ls[h] = (p[0] + p[1]) + (p[2] + p[3]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          pb[t][2 * h + i] = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(p[2 * i]), static_cast<__bf16>(p[2 * i + 1])});
+      }
+      l_run[t] += ls[0] + ls[1];
+    }
+    if (masked) {
+      uint32_t bad = 0;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
         const u32x4 w = __builtin_bit_cast(u32x4, vf[c]);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           bad |= uint32_t((w[e] & 0x7f80u) == 0x7f80u) | uint32_t((w[e] & 0x7f800000u) == 0x7f800000u);
       }
-    }
-    if (MASKED && __any(bad)) {
-      // An infinite V, or NaN, must not reach rows that do not see its key (0 times infinity is NaN): such elements are taken out of
-      // the product and added key by key where the weight is not zero.
-      const int i0 = find.uniform(t0);
+      if (__any(bad)) {
+        // An infinite V, or NaN, must not reach rows that do not see its key (0 times infinity is NaN): such elements are taken out
+        // of the product and added key by key where the weight is not zero.
+        const int i0 = find.uniform(t0);
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < 4; ++i)
 #pragma unroll 1
-          for (int from = 0; from < 4; ++from) {
-            const int vk = min(t0 + 16 * h + 4 * from + i, n_total - 1), r = find.from(i0, vk);
-            const __bf16 *v = reinterpret_cast<const __bf16 *>(tab.v[r] + int64_t(vk - tab.cum[r]) * tab.stride[r]);
+            for (int from = 0; from < 4; ++from) {
+              const int vk = min(t0 + 16 * h + 4 * from + i, n_total - 1), r = find.from(i0, vk);
+              const char *v = tab.v[r] + int64_t(vk - tab.cum[r]) * tab.stride[r] + 8 * q;
 #pragma unroll
-            for (int t = 0; t < RT; ++t) {
-              const float p = __shfl(static_cast<float>(pb[t][4 * h + i]), 16 * from + l16);
+              for (int c = 0; c < NC; ++c) {
+                const bf16x4 x4 = *global_ptr<bf16x4>(v + 32 * c);
 #pragma unroll
-              for (int c = 0; c < NC; ++c)
+                for (int t = 0; t < RT; ++t) {
+                  const uint32_t w = __shfl(pb[t][2 * h + i / 2], 16 * from + l16);
+                  const float p = i & 1 ? bf16_hi(w) : bf16_lo(w);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const float x = static_cast<float>(v[16 * c + 4 * q + e]);
-                  if (not_finite(x) && p != 0.f) o[t][c][e] += p * x;
+                  for (int e = 0; e < 4; ++e) {
+                    const float x = static_cast<float>(x4[e]);
+                    if (not_finite(x) && p != 0.f) o[t][c][e] += p * x;
+                  }
                 }
+              }
             }
-          }
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (not_finite(static_cast<float>(vf[c][e]))) vf[c][e] = static_cast<__bf16>(0.f);
+          for (int e = 0; e < 8; ++e)
+            if (not_finite(static_cast<float>(vf[c][e]))) vf[c][e] = static_cast<__bf16>(0.f);
+      }
     }
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int t = 0; t < RT; ++t) o[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[c], pb[t], o[t][c], 0, 0, 0);
-  };
-  auto compute = [&](int s, int slot) {
-    const int t0 = key0 + 32 * s;
-    if (t0 + 32 > old) step(t0, slot, std::true_type{});
-    else step(t0, slot, std::false_type{});
+      for (int t = 0; t < RT; ++t) o[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[c], __builtin_bit_cast(bf16x8, pb[t]), o[t][c], 0, 0, 0);
   };
 
-  if constexpr (SHARED) {
-    if (n_steps > 0) issue(0, 0);
-    for (int s = 0; s < n_steps; ++s) {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();                             // stage s is there, and nobody reads the other slot any more
-      if (s + 1 < n_steps) issue(s + 1, (s + 1) & 1);
-      compute(s, s & 1);
-    }
-  } else {
-    // two stages of this wave are in flight whenever it waits
-    if (wave < n_steps) issue(wave, 0);
-    if (wave + NW < n_steps) issue(wave + NW, 1);
-    int slot = 0;
-    for (int s = wave; s < n_steps; s += NW, slot ^= 1) {
-      if (s + NW < n_steps) {
-        if constexpr (BIAS) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(MINE + 1) : "memory");
-        else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(MINE) : "memory");
-      } else {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      }
-      compute(s, slot);
+  // RW waves: NS - 1 stages are on their way when a step begins; one wave: NS when it waits
+  constexpr int AHEAD = RW > 1 ? NS - 1 : NS;
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (ks + i * KS < n_steps) issue(ks + i * KS, i);
+  find_masks(pd, n, up_here, row0, rows);
+  // the stages behind the one that is waited for: what the wave that also fetches positions has in flight is more, never less
+  constexpr int LATER = (AHEAD - 1) * (RW > 1 ? MINE : MINE + (BIAS ? 1 : 0));
+  int slot = 0;
+  for (int s0 = 0; s0 < n_steps; s0 += KS) {
+    const int s = s0 + ks;
+    if (s + (AHEAD - 1) * KS < n_steps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LATER) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if constexpr (RW > 1) {
+      __syncthreads();                             // this stage is there, and nobody reads the slot of the one before any more
+      if (s + AHEAD * KS < n_steps) issue(s + AHEAD * KS, slot == 0 ? NS - 1 : slot - 1);
+      if (s < n_steps) compute(s, slot);
+    } else {
+      if (s < n_steps) compute(s, slot);
       // the reads of this slot have returned before the next stage may overwrite it
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if (s + 2 * NW < n_steps) issue(s + 2 * NW, slot);
+      if (s + AHEAD * KS < n_steps) issue(s + AHEAD * KS, slot);
     }
+    slot = slot + 1 == NS ? 0 : slot + 1;
   }
 #pragma unroll
   for (int t = 0; t < RT; ++t) l_run[t] = rows_sum(l_run[t]);
-  finish<__bf16, D, RT, KEYS>(pd, d, b, rows, m_run, l_run, reinterpret_cast<float *>(ring), [&](int t, auto &&fn) {
-#pragma unroll
-    for (int c = 0; c < NC; ++c) fn(16 * c + 4 * q, o[t][c]);
-  });
+  finish<__bf16, D, RT, RW, KS>(pd, d, b, g, n, rows, m_run, l_run, o, reinterpret_cast<float *>(ring), [&](int c) { return 16 * c + 4 * q; });
 }
 
 // fp32 on v_mfma_f32_16x16x4_f32, 16 keys a step, everything in 32 bits; K and V come from memory straight into registers.
 //   S^T[key, row] = K[key, :] . Q[row, :]       slots bound to dims 16 i + 4 (L / 16) + e
 //   O^T[d, row]  += V^T[d, key] . P^T[key, row] slot L / 16 of step r bound to key 4 (L / 16) + r; rows of O^T to dims 64 h + 4 (L % 16) + c
 // Sums are kept in short chains that are added up (a single chain of D products rounds several times as much).
-template <int D, int RT, int NW, bool BIAS>
-__global__ __launch_bounds__(64 * NW) void tree_f32_kernel(PlanDev pd, TreeDev d) {
+template <int D, int RT, int KS, bool BIAS>
+__global__ __launch_bounds__(64 * KS, 2) void tree_f32_kernel(PlanDev pd, TreeDev d) {
   constexpr int NI = D / 16, NH = D / 64;
-  __shared__ __attribute__((aligned(16))) float merge[NW > 1 ? NW * RT * 16 * (D + 4) : 4];
+  __shared__ __attribute__((aligned(16))) float merge[KS > 1 ? (KS - 1) * RT * 16 * (D + 4) : 4];
   __shared__ KeyTable tab;
   const TreeArgs &a = d.a;
   const int Hq = pd.n_q_heads, Hkv = pd.n_kv_heads, G = Hq / Hkv;
   const int b = blockIdx.x / Hkv, g = blockIdx.x % Hkv;
   const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const RespRows rr = resp_rows(a, b);
   const int n = a.n_nodes ? min(max(a.n_nodes[b], 0), a.max_nodes) : a.max_nodes;
+  if (blockIdx.y == gridDim.y - 1) {
+    if (blockIdx.z == 0) append_nodes<float, D>(pd, a, b, g, rr.write, n);
+    return;
+  }
   const int row0 = int(blockIdx.y) * 16 * RT;
-  if (row0 >= n * G) return;
 
   Rows<RT> rows;
-  find_rows<RT, BIAS>(pd, a, b, g, n, row0, rows);
+  find_rows<RT, BIAS>(pd, a, b, g, row0, rows);
+  const int up = load_parent(a, b);
   float qf[RT][4 * NI];
   const float scale2 = a.scale * kLog2e;
 #pragma unroll
@@ -455,8 +559,7 @@ __global__ __launch_bounds__(64 * NW) void tree_f32_kernel(PlanDev pd, TreeDev d
       for (int e = 0; e < 4; ++e) qf[t][4 * i + e] = v[e] * scale2;
     }
   }
-  const RespRows rr = resp_rows(a, b);
-  if (blockIdx.y == 0 && blockIdx.z == 0) append_nodes<float, D>(pd, a, b, g, rr.write, n);
+  if (row0 >= n * G) return;
   build_key_table<float, D>(pd, a, b, g, rr.read, NewKeys{b * a.max_nodes, n, int64_t(Hkv) * D * 4}, BIAS, tab);
   const RangeSearch find(tab);
   const int n_total = tab.n_total, old = n_total - n;
@@ -598,95 +701,110 @@ __global__ __launch_bounds__(64 * NW) void tree_f32_kernel(PlanDev pd, TreeDev d
     if (t0 + 16 > old) step(t0, st, std::true_type{});
     else step(t0, st, std::false_type{});
   };
-  for (int t0 = key0 + 16 * wave; t0 < key1; t0 += 16 * NW) {
-    Stage st;
-    load(t0, st);
-    compute(t0, st);
+  // the loads of a step leave before the arithmetic of the one before
+  constexpr int STEP = 16 * KS;
+  Stage s0, s1;
+  int t0 = key0 + 16 * wave;
+  if (t0 < key1) load(t0, s0);
+  find_masks(pd, n, up, row0, rows);
+  while (t0 < key1) {
+    if (t0 + STEP < key1) load(t0 + STEP, s1);
+    compute(t0, s0);
+    t0 += STEP;
+    if (t0 >= key1) break;
+    if (t0 + STEP < key1) load(t0 + STEP, s0);
+    compute(t0, s1);
+    t0 += STEP;
   }
 #pragma unroll
   for (int t = 0; t < RT; ++t) l_run[t] = rows_sum(l_run[t]);
-  finish<float, D, RT, NW>(pd, d, b, rows, m_run, l_run, merge, [&](int t, auto &&fn) {
+  f32x4 ov[RT][NI];                  // [4h + r]: four dims from 64h + 16 q + 4r on
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
 #pragma unroll
     for (int h = 0; h < NH; ++h)
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        fn(64 * h + 16 * q + 4 * r, f32x4{o[t][4 * h][r], o[t][4 * h + 1][r], o[t][4 * h + 2][r], o[t][4 * h + 3][r]});
-  });
+      for (int r = 0; r < 4; ++r) ov[t][4 * h + r] = f32x4{o[t][4 * h][r], o[t][4 * h + 1][r], o[t][4 * h + 2][r], o[t][4 * h + 3][r]};
+  finish<float, D, RT, 1, KS>(pd, d, b, g, n, rows, m_run, l_run, ov, merge, [&](int i) { return 64 * (i / 4) + 16 * q + 4 * (i % 4); });
 }
 
-// Adds up the pieces of a row in their order: a thread per four dims.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void tree_merge_kernel(PlanDev pd, TreeDev d) {
-  constexpr int PER = D / 4;
-  const int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x, row = at / PER;
-  if (row >= d.rows) return;
-  const int dim = int(at % PER) * 4;
-  if (d.a.n_nodes) {
-    const int64_t node = row / pd.n_q_heads;
-    if (node % d.a.max_nodes >= d.a.n_nodes[node / d.a.max_nodes]) return;
+// How a launch is shared out, a function of the call's sizes alone.  Measured, bf16, 128 dims, us for one layer (~500 keys, 32 KV
+// heads; 950 keys with 8), by waves that take different keys / different rows:
+//   up to 16 rows to a KV head, 6 / 8 / 10 / 16 / 20 / 32 prompts: 1 wave 29 / 29 / 32 / 36 / 43 / 55, 2 key groups
+//     20 / 22 / 27 / 31 / 48 / 60, 4 key groups 18 / 20 / 32 / 39 / 50 / 73
+//   60 rows, 4 / 8 / 16 / 32 prompts: 2 row waves 31 / 33 / 46 / 89, times 2 key groups 27 / 30 / 63 / 127, times 4 21 / 26 / 58 / 112
+//   256 rows, 4 / 8 / 16 / 32 prompts of 8 KV heads: 2 row waves times 4 key groups 24 / 26 / 49 / 116, 4 times 2 31 / 32 / 35 / 76,
+//     4 row waves 39 / 39 / 41 / 60
+// Hence: as many key groups as leave a workgroup to every compute unit (their slots fill its LDS), none where there are more
+// workgroups than that; four waves to share a stage once two would give more workgroups than compute units.
+// Lists are cut into pieces of at least a step for every key group where that still leaves compute units without a workgroup.
+struct TreeShape {
+  int rt, rw, ks, blocks, pieces;
+};
+static TreeShape tree_shape(const sp_plan *plan, int max_nodes, int64_t keys, int64_t part_rows, int n_cu) {
+  const int G = plan->n_q_heads / plan->n_kv_heads, rows = max_nodes * G;
+  const int64_t pairs = int64_t(plan->n_prompts) * plan->n_kv_heads;
+  TreeShape t{rows <= 16 ? 1 : 2, 1, 1, 1, 1};
+  auto wgs = [&]() {
+    t.blocks = (rows + 16 * t.rt * t.rw - 1) / (16 * t.rt * t.rw);
+    return pairs * t.blocks;
+  };
+  if (plan->dtype == SP_BF16) {
+    if (rows > 32) t.rw = 2;
+    if (rows > 64 && wgs() > n_cu) t.rw = 4;
+    const int64_t n = wgs();
+    if (n <= n_cu) t.ks = t.rw == 4 ? 2 : 4;
+    else if (n <= 2 * n_cu && t.rw == 1) t.ks = 2;
+  } else {
+    t.rt = 1;
+    t.ks = 4;
   }
-  const float *ml = d.part + d.n_pieces * d.rows * D;
-  float m = kNegBig, l = 0.f;
-  f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  for (int p = 0; p < d.n_pieces; ++p) {
-    const int64_t i = p * d.rows + row;
-    const float pm = ml[2 * i], pl = ml[2 * i + 1], m_new = fmaxf(m, pm), wa = fast_exp2(m - m_new), wb = fast_exp2(pm - m_new);
-    const f32x4 x = *reinterpret_cast<const f32x4 *>(d.part + i * D + dim);
-    l = l * wa + pl * wb;
-    m = m_new;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = v[e] * wa + x[e] * wb;
+  const int64_t n = wgs();
+  if (n <= kTreeCounters) {
+    int64_t p = std::min<int64_t>(n_cu / n, (keys + 16 * t.ks) / (32 * t.ks));
+    p = std::min<int64_t>(p, int64_t(kTreePartBytes) / (part_rows * (plan->head_dim + 2) * 4));
+    t.pieces = int(std::max<int64_t>(p, 1));
   }
-  store4<T, D>(d, row, dim, v, 1.f / l);
+  return t;
 }
 
 template <typename T, int D>
-static hipError_t launch_tree(const sp_plan *plan, TreeDev &d, int64_t keys, hipStream_t s, bool *no_scratch) {
-  constexpr bool kBf16 = sizeof(T) == 2;
-  const int G = plan->n_q_heads / plan->n_kv_heads, rows = d.a.max_nodes * G, pairs = plan->n_prompts * plan->n_kv_heads;
-  const int n_cu = plan->ctx->n_cu;
-  int rt = rows <= 16 ? 1 : 2;
-  int nw = 4;
-  bool shared = kBf16 && rows > 64;
-  const int block_rows = 16 * rt * (shared ? nw : 1);
-  const int blocks = (rows + block_rows - 1) / block_rows;
-  d.n_pieces = 1;
-  const int64_t wgs = int64_t(pairs) * blocks;
-  int64_t pieces = std::min<int64_t>((n_cu + wgs - 1) / wgs, keys / 256);
-  pieces = std::min<int64_t>(pieces, int64_t(kTreePartBytes) / (d.rows * (D + 2) * 4));
-  if (pieces > 1) {
-    d.part = static_cast<float *>(tree_scratch(plan, s));
-    if (!d.part) { *no_scratch = true; return hipSuccess; }
-    d.n_pieces = int(pieces);
-  }
-  d.a.few_wgs = wgs * d.n_pieces <= int64_t(kDecFewWgsPerCu) * n_cu;
-  const dim3 grid(static_cast<unsigned>(pairs), static_cast<unsigned>(blocks), static_cast<unsigned>(d.n_pieces)), block(64u * unsigned(nw));
+static hipError_t launch_tree(const sp_plan *plan, TreeDev &d, const TreeShape &t, hipStream_t s) {
+  const int64_t pairs = int64_t(plan->n_prompts) * plan->n_kv_heads;
+  const dim3 grid(static_cast<unsigned>(pairs), unsigned(t.blocks) + 1, unsigned(t.pieces)), block(64u * unsigned(t.rw * t.ks));
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, plan->dev, d); };
   auto pick = [&](auto bias) {
     constexpr bool BIAS = decltype(bias)::value;
-    if constexpr (kBf16) {
-      if (shared) go(tree_bf16_kernel<D, 2, 4, true, BIAS>);
-      else if (rt == 1) go(tree_bf16_kernel<D, 1, 4, false, BIAS>);
-      else go(tree_bf16_kernel<D, 2, 4, false, BIAS>);
-    } else {
-      if (rt == 1) go(tree_f32_kernel<D, 1, 4, BIAS>);
-      else go(tree_f32_kernel<D, 2, 4, BIAS>);
-    }
+    if constexpr (sizeof(T) == 4) go(tree_f32_kernel<D, 1, 4, BIAS>);
+    else if (t.rw == 4) t.ks == 2 ? go(tree_bf16_kernel<D, 2, 4, 2, 4, BIAS>) : go(tree_bf16_kernel<D, 2, 4, 1, 3, BIAS>);
+    else if (t.rw == 2) t.ks == 4 ? go(tree_bf16_kernel<D, 2, 2, 4, 2, BIAS>) : go(tree_bf16_kernel<D, 2, 2, 1, 2, BIAS>);
+    else if (t.rt == 1) t.ks == 4 ? go(tree_bf16_kernel<D, 1, 1, 4, 2, BIAS>) : t.ks == 2 ? go(tree_bf16_kernel<D, 1, 1, 2, 2, BIAS>)
+                                                                                          : go(tree_bf16_kernel<D, 1, 1, 1, 2, BIAS>);
+    else t.ks == 4 ? go(tree_bf16_kernel<D, 2, 1, 4, 2, BIAS>) : t.ks == 2 ? go(tree_bf16_kernel<D, 2, 1, 2, 2, BIAS>)
+                                                                           : go(tree_bf16_kernel<D, 2, 1, 1, 2, BIAS>);
   };
   if (plan->has_slopes) pick(std::true_type{}); else pick(std::false_type{});
-  if (d.n_pieces > 1)
-    hipLaunchKernelGGL((tree_merge_kernel<T, D>), dim3(unsigned((d.rows * (D / 4) + 255) / 256)), dim3(256), 0, s, plan->dev, d);
   return hipGetLastError();
 }
 
 hipError_t launch_tree_decode(const sp_plan *plan, const TreeArgs &a, hipStream_t s, bool *no_scratch) {
-  TreeDev d{a, 1, nullptr, int64_t(plan->n_prompts) * a.max_nodes * plan->n_q_heads};
+  TreeDev d{a, 1, nullptr, int64_t(plan->n_prompts) * a.max_nodes * plan->n_q_heads, nullptr};
   const int64_t resp = int64_t(a.resp_len_add) + (a.resp_len ? a.resp_capacity / 2 : 0);
   const int64_t keys = plan->max_shared_keys + int64_t(a.k) * plan->max_path_keys + std::min<int64_t>(resp, a.resp_capacity);
+  const int n_cu = plan->ctx->n_cu;
+  const TreeShape t = tree_shape(plan, a.max_nodes, keys, d.rows, n_cu);
   *no_scratch = false;
+  d.n_pieces = t.pieces;
+  if (t.pieces > 1) {
+    const DecodeRegion *region = tree_region(plan, s);
+    if (!region) { *no_scratch = true; return hipSuccess; }
+    d.part = static_cast<float *>(region->part);
+    d.count = region->count;
+  }
+  d.a.few_wgs = int64_t(plan->n_prompts) * plan->n_kv_heads * t.blocks * t.pieces <= int64_t(kDecFewWgsPerCu) * n_cu;
   if (plan->dtype == SP_BF16)
-    return plan->head_dim == 128 ? launch_tree<__bf16, 128>(plan, d, keys, s, no_scratch) : launch_tree<__bf16, 64>(plan, d, keys, s, no_scratch);
-  return plan->head_dim == 128 ? launch_tree<float, 128>(plan, d, keys, s, no_scratch) : launch_tree<float, 64>(plan, d, keys, s, no_scratch);
+    return plan->head_dim == 128 ? launch_tree<__bf16, 128>(plan, d, t, s) : launch_tree<__bf16, 64>(plan, d, t, s);
+  return plan->head_dim == 128 ? launch_tree<float, 128>(plan, d, t, s) : launch_tree<float, 64>(plan, d, t, s);
 }
 
 }  // namespace sp

@@ -1,6 +1,8 @@
 """sp_sample against the 64-bit oracle.  Tokens are equal wherever the oracle's decision is further from its border than the
 weights' resolution: a weight is off by 2^-(62 - b) of the largest, b bits of the vocabulary, a sum of all by 2^(2 b - 62) at most
 (four times that is asked for, and at least 2^-45, where the oracle's own sums of doubles end)."""
+import gc
+
 import numpy as np
 import pytest
 import torch
@@ -18,6 +20,7 @@ pytestmark = pytest.mark.gpu
 def ctx():
     c = B.Context(0)
     yield c
+    gc.collect()                                            # plans in reference cycles go now, and not in some later capture
     c.close()
 
 

@@ -1,4 +1,6 @@
 """sp_tree_accept against the oracle's walk, with every byte of the caches compared."""
+import gc
+
 import numpy as np
 import pytest
 import torch
@@ -16,6 +18,7 @@ pytestmark = pytest.mark.gpu
 def ctx():
     c = B.Context(0)
     yield c
+    gc.collect()                                            # plans in reference cycles go now, and not in some later capture
     c.close()
 
 

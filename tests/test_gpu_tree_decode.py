@@ -1,4 +1,6 @@
 """sp_tree_decode against the 64-bit oracle: types, head layouts, lengths, trees, what is left alone, refusals, graphs, streams."""
+import gc
+
 import numpy as np
 import pytest
 import torch
@@ -15,6 +17,7 @@ pytestmark = pytest.mark.gpu
 def ctx():
     c = B.Context(0)
     yield c
+    gc.collect()                                            # plans in reference cycles go now, and not in some later capture
     c.close()
 
 
