@@ -209,55 +209,83 @@ __device__ __forceinline__ void finish(const PlanDev &pd, const TreeDev &d, int 
   // a thread per row and four dims
   constexpr int PER = D / 4;
   const int G = pd.n_q_heads / pd.n_kv_heads, row0 = int(blockIdx.y) * RW * RT * 16, rows = min(RW * RT * 16, n * G - row0);
-  for (int i = threadIdx.x; i < rows * PER; i += 64 * RW * KS) {
-    const int rr = row0 + i / PER, at_dim = i % PER * 4;
-    const int64_t row = base + int64_t(rr / G) * pd.n_q_heads + g * G + rr % G;
-    float mm = kNegBig, ll = 0.f;
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    for (int p0 = 0; p0 < d.n_pieces; p0 += 4) {     // four pieces' loads in flight
-      f32x4 x[4];
-      uint64_t w[4];
+  constexpr int NT = 64 * RW * KS;
+  auto merge = [&](auto items) {                     // as many of a thread's at once, with four pieces' loads each
+    constexpr int U = decltype(items)::value;
+    for (int i0 = threadIdx.x; i0 < rows * PER; i0 += U * NT) {
+      int64_t row[U];
+      int at_dim[U];
+      float mm[U], ll[U];
+      f32x4 v[U];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int64_t at = min(p0 + j, d.n_pieces - 1) * d.rows + row;
-        x[j] = load_shared(d.part + at * D + at_dim);
-        w[j] = __hip_atomic_load(reinterpret_cast<unsigned long long *>(part_ml + 2 * at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      for (int u = 0; u < U; ++u) {
+        const int i = min(i0 + u * NT, rows * PER - 1), rr = row0 + i / PER;
+        at_dim[u] = i % PER * 4;
+        row[u] = base + int64_t(rr / G) * pd.n_q_heads + g * G + rr % G;
+        mm[u] = kNegBig;
+        ll[u] = 0.f;
+        v[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      for (int p0 = 0; p0 < d.n_pieces; p0 += 4) {
+        f32x4 x[U][4];
+        uint64_t w[U][4];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int64_t at = min(p0 + j, d.n_pieces - 1) * d.rows + row[u];
+            x[u][j] = load_shared(d.part + at * D + at_dim[u]);
+            w[u][j] = __hip_atomic_load(reinterpret_cast<unsigned long long *>(part_ml + 2 * at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if (p0 + j >= d.n_pieces) break;
+            const float pm = __uint_as_float(uint32_t(w[u][j])), pl = __uint_as_float(uint32_t(w[u][j] >> 32));
+            const float m_new = fmaxf(mm[u], pm), wa = fast_exp2(mm[u] - m_new), wb = fast_exp2(pm - m_new);
+            ll[u] = ll[u] * wa + pl * wb;
+            mm[u] = m_new;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[u][e] = v[u][e] * wa + x[u][j][e] * wb;
+          }
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (p0 + j >= d.n_pieces) break;
-        const float pm = __uint_as_float(uint32_t(w[j])), pl = __uint_as_float(uint32_t(w[j] >> 32));
-        const float m_new = fmaxf(mm, pm), wa = fast_exp2(mm - m_new), wb = fast_exp2(pm - m_new);
-        ll = ll * wa + pl * wb;
-        mm = m_new;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = v[e] * wa + x[j][e] * wb;
-      }
-    }
-    store4<T, D>(d, row, at_dim, v, 1.f / ll);
+      for (int u = 0; u < U; ++u)
+        if (i0 + u * NT < rows * PER) store4<T, D>(d, row[u], at_dim[u], v[u], 1.f / ll[u]);
+    }  };
+    if (rows * PER <= NT) merge(std::integral_constant<int, 1>{});
+    else merge(std::integral_constant<int, 2>{});
   }
-}
 
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 
 }  // namespace
 
-// bf16 on v_mfma_f32_16x16x32_bf16.  Per step of 32 keys (two tiles of 16):
+// A step is 32 keys in bf16 (two tiles of 16), 16 in fp32.
+// bf16, v_mfma_f32_16x16x32_bf16:
 //   S^T[key, row]  = K[key, :] . Q[row, :]         A = K (LDS), B = Q (registers)
 //   O^T[d, row]   += V^T[d, key] . P^T[key, row]   A = V (LDS, transpose reads), B = P as it is
 // In the accumulator lane L holds row L % 16 and keys 4 (L / 16) + i of each tile, which are bound to the k-slots that the lane feeds in
 // the second product.  P is rounded to bf16 there, as the output is (the sum of the weights is not); that is half a step of every weight, and the
 // result is as far off as two roundings of it instead of one.
+// fp32, v_mfma_f32_16x16x4_f32, everything in 32 bits:
+//   S^T[key, row] = K[key, :] . Q[row, :]       slots bound to dims 16 i + 4 (L / 16) + e
+//   O^T[d, row]  += V^T[d, key] . P^T[key, row] slot L / 16 of product r bound to key 4 (L / 16) + r; rows of O^T to dims 64 h + 4 (L % 16) + c
+// Sums are kept in short chains that are added up (a single chain of D products rounds several times as much).
 // RW waves take different rows and fill each stage together; KS such groups take every KS-th step and have slots of their own.
-template <int D, int RT, int RW, int KS, int NS, bool BIAS>
-__global__ __launch_bounds__(64 * RW * KS, 2) void tree_bf16_kernel(PlanDev pd, TreeDev d) {
-  constexpr int ROWB = D * 2, CPR = D / 8, RPC = 256 / ROWB, RG = 64 / CPR;   // LDS row, its 16-byte chunks, rows per 256 bytes, rows per DMA
-  constexpr int HALFB = 32 * ROWB, SLOTB = 2 * HALFB;
-  constexpr int NI = 32 / RG;                    // DMA instructions per half
+template <typename T, int D, int RT, int RW, int KS, int NS, bool BIAS>
+__global__ __launch_bounds__(64 * RW * KS, 2) void tree_kernel(PlanDev pd, TreeDev d) {
+  constexpr bool kBf16 = sizeof(T) == 2;
+  constexpr int STEP = kBf16 ? 32 : 16;
+  constexpr int ROWB = D * int(sizeof(T)), CPR = ROWB / 16, RG = 64 / CPR;    // LDS row, its 16-byte chunks, rows per DMA
+  constexpr int RPC = ROWB < 256 ? 256 / ROWB : 1;                            // rows per 256 bytes (all banks)
+  constexpr int HALFB = STEP * ROWB, SLOTB = 2 * HALFB;
+  constexpr int NI = STEP / RG;                  // DMA instructions per half
   constexpr bool STREAM = RW == 1;               // one block of rows: nobody else reads these keys
   constexpr int RINGB = NS * SLOTB * KS;
   constexpr int MERGEB = (KS - 1) * RW * RT * 16 * (D + 4) * 4;
-  constexpr int NJ = D / 32, NC = D / 16;
+  constexpr int NQ = CPR / 4, NC = D / 16;       // 16-byte vectors of a row per lane; output vectors
   __shared__ __attribute__((aligned(1024))) unsigned char ring[RINGB > MERGEB ? RINGB : MERGEB];
   __shared__ __attribute__((aligned(256))) float s_pos[BIAS ? NS * KS : 1][64];
   __shared__ KeyTable tab;
@@ -269,7 +297,7 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void tree_bf16_kernel(PlanDev pd, 
   const RespRows rr = resp_rows(a, b);
   const int n = a.n_nodes ? min(max(a.n_nodes[b], 0), a.max_nodes) : a.max_nodes;
   if (blockIdx.y == gridDim.y - 1) {
-    if (blockIdx.z == 0) append_nodes<__bf16, D>(pd, a, b, g, rr.write, n);
+    if (blockIdx.z == 0) append_nodes<T, D>(pd, a, b, g, rr.write, n);
     return;
   }
   const int row0 = (int(blockIdx.y) * RW + rw) * 16 * RT;
@@ -277,34 +305,34 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void tree_bf16_kernel(PlanDev pd, 
   Rows<RT> rows;
   find_rows<RT, BIAS>(pd, a, b, g, row0, rows);
   const int up = load_parent(a, b);
-  bf16x8 qf[RT][NJ];
+  u32x4 qf[RT][NQ];
 #pragma unroll
   for (int t = 0; t < RT; ++t)
 #pragma unroll
-    for (int j = 0; j < NJ; ++j)
-      qf[t][j] = *reinterpret_cast<const bf16x8 *>(static_cast<const __bf16 *>(a.q_new) +
-                                                   (((int64_t)b * a.max_nodes + rows.node[t]) * Hq + rows.head[t]) * D + (q + 4 * j) * 8);
+    for (int j = 0; j < NQ; ++j)
+      qf[t][j] = ld16(static_cast<const T *>(a.q_new) + (((int64_t)b * a.max_nodes + rows.node[t]) * Hq + rows.head[t]) * D +
+                      (q + 4 * j) * (16 / int(sizeof(T))));
   const float scale2 = a.scale * kLog2e;
   if (int(blockIdx.y) * RW * 16 * RT >= n * G) return;
-  build_key_table<__bf16, D>(pd, a, b, g, rr.read, NewKeys{b * a.max_nodes, n, int64_t(Hkv) * D * 2}, BIAS, tab);
+  build_key_table<T, D>(pd, a, b, g, rr.read, NewKeys{b * a.max_nodes, n, int64_t(Hkv) * ROWB}, BIAS, tab);
   const RangeSearch find(tab);
   // The compiler waits for a load of its own at the first use, which would be in the loop, with all the DMA in flight there.
 #pragma unroll
   for (int t = 0; t < RT; ++t)
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(qf[t][j]));
+    for (int j = 0; j < NQ; ++j) asm volatile("" : "+v"(qf[t][j]));
   int up_here = up;
   asm volatile("" : "+v"(up_here));
   const int n_total = tab.n_total, old = n_total - n;
-  // pieces are multiples of 32 keys, so that only steps at the end of the list reach beyond it
-  const int piece = ((n_total + d.n_pieces - 1) / d.n_pieces + 31) & ~31;
+  // pieces are multiples of a step, so that only steps at the end of the list reach beyond it
+  const int piece = ((n_total + d.n_pieces - 1) / d.n_pieces + STEP - 1) & ~(STEP - 1);
   const int key0 = min(int(blockIdx.z) * piece, n_total), key1 = min(key0 + piece, n_total);
-  const int n_steps = (key1 - key0 + 31) / 32;
+  const int n_steps = (key1 - key0 + STEP - 1) / STEP;
 
   // LDS rows are unpadded; the 16-byte chunks of a row are swizzled on the global side, so that row reads of K (16 rows, one
-  // chunk) and transpose reads of V (8 rows of one chunk pair at a time) spread over the banks.
-  auto fK = [](int row) { return (row / RPC) % CPR; };
-  auto fV = [](int row) { return ((row / RPC) % (CPR / 4)) * 4 | ((row >> 2) & 1) * 2; };
+  // chunk) and, in bf16, transpose reads of V (8 rows of one chunk pair at a time) spread over the banks.
+  auto fK = [](int row) { return (row / RPC) % (CPR < 16 ? CPR : 16); };
+  auto fV = [](int row) { return kBf16 ? ((row / RPC) % (CPR / 4)) * 4 | ((row >> 2) & 1) * 2 : 0; };
   const uint32_t ring_base = (uint32_t)(size_t)(lds_byte *)ring + ks * NS * SLOTB;
   const uint32_t pos_base = (uint32_t)(size_t)(lds_byte *)&s_pos[0][0] + ks * NS * 256;
   const unsigned char *ringp = ring + ks * NS * SLOTB;
@@ -312,16 +340,24 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void tree_bf16_kernel(PlanDev pd, 
   static_assert(2 * NI % RW == 0, "the waves of a group share a stage evenly");
   constexpr int MINE = 2 * NI / RW;              // DMA instructions of a wave per stage
 
+  // the range that the last stage began in, wave-uniform: looking it up takes longer than the requests
+  int c0 = 0, c1 = 0, i0 = 0;
+  int64_t stride = 0;
+  const char *k0 = nullptr, *v0 = nullptr;
   auto issue = [&](int s, int slot) {
-    const int t0 = key0 + 32 * s;
-    const int i0 = find.uniform(t0);
-    const int c0 = __builtin_amdgcn_readfirstlane(tab.cum[i0]), c1 = __builtin_amdgcn_readfirstlane(tab.cum[i0 + 1]);
-    const int64_t stride = uniform64(tab.stride[i0]);
+    const int t0 = key0 + STEP * s;
     const uint32_t lds = ring_base + slot * SLOTB;
+    if (t0 >= c1) {
+      i0 = find.uniform(t0);
+      c0 = __builtin_amdgcn_readfirstlane(tab.cum[i0]);
+      c1 = __builtin_amdgcn_readfirstlane(tab.cum[i0 + 1]);
+      stride = uniform64(tab.stride[i0]);
+      k0 = reinterpret_cast<const char *>(uniform64(reinterpret_cast<int64_t>(tab.k[i0])));
+      v0 = reinterpret_cast<const char *>(uniform64(reinterpret_cast<int64_t>(tab.v[i0])));
+    }
     // rows RG m .. of the half: consecutive tokens of one range, or each row looked up by itself (past the end: the last key again)
-    const bool plain = t0 + 32 <= c1 && stride < (int64_t(1) << 27);
-    const char *kb = reinterpret_cast<const char *>(uniform64(reinterpret_cast<int64_t>(tab.k[i0]))) + (t0 - c0) * stride;
-    const char *vb = reinterpret_cast<const char *>(uniform64(reinterpret_cast<int64_t>(tab.v[i0]))) + (t0 - c0) * stride;
+    const bool plain = t0 + STEP <= c1 && stride < (int64_t(1) << 27);
+    const char *kb = k0 + (t0 - c0) * stride, *vb = v0 + (t0 - c0) * stride;
     const uint32_t row_off = uint32_t(drow) * uint32_t(stride);
     if (plain) {
 #pragma unroll
@@ -344,7 +380,7 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void tree_bf16_kernel(PlanDev pd, 
       }
     }
     if (BIAS && rw == 0) {
-      const int vk = min(t0 + (lane & 31), n_total - 1), i = find.from(i0, vk);
+      const int vk = min(t0 + (lane & (STEP - 1)), n_total - 1), i = find.from(i0, vk);
       dma4(tab.pos[i] + (vk - tab.cum[i]), pos_base + slot * 256);
     }
   };
@@ -360,10 +396,43 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void tree_bf16_kernel(PlanDev pd, 
   }
   const int tr_row = l16 >> 2, tr_x = (lane & 3) >> 1, tr_sub8 = (lane & 1) * 8;
 
+  // bit k: the row of tile t sees key t0 + k (all keys before the nodes)
+  auto seen = [&](int t, int t0) {
+    const int at = t0 - old;
+    return at >= 0 ? uint32_t(rows.mask[t] >> at) : uint32_t(rows.mask[t]) << -at | ((1u << -at) - 1);
+  };
+  // An infinite V, or NaN, must not reach rows that do not see its key (0 times infinity is NaN).  Steps with nodes look for such
+  // elements, take them out of the product and add them key by key where the weight is not zero: weight(t, i) is that of key
+  // 4 (L / 16) + i of the keys from t0 on, dim(c, e) the place of o[t][c][e].
+  auto add_infinite = [&](int t0, auto &&weight, auto &&dim) {
+    const int i0 = find.uniform(t0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll 1
+      for (int from = 0; from < 4; ++from) {
+        const int vk = min(t0 + 4 * from + i, n_total - 1), r = find.from(i0, vk);
+        const char *v = tab.v[r] + int64_t(vk - tab.cum[r]) * tab.stride[r];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          const float p = __shfl(weight(t, i), 16 * from + l16);
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float x = static_cast<float>(*global_ptr<T>(v + dim(c, e) * sizeof(T)));
+              o[t][c][e] += not_finite(x) && p != 0.f ? p * x : 0.f;
+            }
+            __builtin_amdgcn_sched_barrier(0);       // few masks at a time: the loop around has no scalar registers to spare
+          }
+        }
+      }
+  };
+
   // one step on a slot
-  auto compute = [&](int step, int slot) {
-    const int t0 = key0 + 32 * step;
-    const bool masked = t0 + 32 > old;               // it holds nodes, or reaches beyond them
+  auto compute_bf16 = [&](int step, int slot) {
+    constexpr int NJ = D / 32;
+    const int t0 = key0 + STEP * step;
+    const bool masked = t0 + STEP > old;             // it holds nodes, or reaches beyond them
     const unsigned char *sl = ringp + slot * SLOTB;
     f32x4 s[RT][2];
 #pragma unroll
@@ -375,7 +444,7 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void tree_bf16_kernel(PlanDev pd, 
         const int row = 16 * h + l16;
         const bf16x8 k = *reinterpret_cast<const bf16x8 *>(sl + row * ROWB + ((4 * j + q) ^ fK(row)) * 16);
 #pragma unroll
-        for (int t = 0; t < RT; ++t) s[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[t][j], s[t][h], 0, 0, 0);
+        for (int t = 0; t < RT; ++t) s[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, __builtin_bit_cast(bf16x8, qf[t][j]), s[t][h], 0, 0, 0);
       }
     bf16x8 vf[NC];                                   // on its way under the softmax
     const unsigned char *vs = sl + HALFB + tr_sub8;
@@ -406,11 +475,9 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void tree_bf16_kernel(PlanDev pd, 
 #pragma unroll
       for (int t = 0; t < RT; ++t) mx[t] = largest(s[t]);
     } else {
-      // bit k of `see`: the row sees key t0 + k (all keys before the nodes)
-      const int at = t0 - old;
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
-        const uint32_t see = (at >= 0 ? uint32_t(rows.mask[t] >> at) : uint32_t(rows.mask[t]) << -at | ((1u << -at) - 1)) >> (4 * q);
+        const uint32_t see = seen(t, t0) >> (4 * q);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -454,43 +521,130 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void tree_bf16_kernel(PlanDev pd, 
           bad |= uint32_t((w[e] & 0x7f80u) == 0x7f80u) | uint32_t((w[e] & 0x7f800000u) == 0x7f800000u);
       }
       if (__any(bad)) {
-        // An infinite V, or NaN, must not reach rows that do not see its key (0 times infinity is NaN): such elements are taken out
-        // of the product and added key by key where the weight is not zero.
-        const int i0 = find.uniform(t0);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
+          add_infinite(t0 + 16 * h, [&](int t, int i) { return i & 1 ? bf16_hi(pb[t][2 * h + i / 2]) : bf16_lo(pb[t][2 * h + i / 2]); },
+                       [&](int c, int e) { return 16 * c + 4 * q + e; });
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll 1
-            for (int from = 0; from < 4; ++from) {
-              const int vk = min(t0 + 16 * h + 4 * from + i, n_total - 1), r = find.from(i0, vk);
-              const char *v = tab.v[r] + int64_t(vk - tab.cum[r]) * tab.stride[r] + 8 * q;
-#pragma unroll
-              for (int c = 0; c < NC; ++c) {
-                const bf16x4 x4 = *global_ptr<bf16x4>(v + 32 * c);
-#pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                  const uint32_t w = __shfl(pb[t][2 * h + i / 2], 16 * from + l16);
-                  const float p = i & 1 ? bf16_hi(w) : bf16_lo(w);
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) {
-                    const float x = static_cast<float>(x4[e]);
-                    if (not_finite(x) && p != 0.f) o[t][c][e] += p * x;
-                  }
-                }
-              }
-            }
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
+        for (int c = 0; c < NC; ++c) {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             if (not_finite(static_cast<float>(vf[c][e]))) vf[c][e] = static_cast<__bf16>(0.f);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     }
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int t = 0; t < RT; ++t) o[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[c], __builtin_bit_cast(bf16x8, pb[t]), o[t][c], 0, 0, 0);
+  };
+
+  auto compute_f32 = [&](int step, int slot) {
+    constexpr int NH = D / 64;
+    const int t0 = key0 + STEP * step;
+    const bool masked = t0 + STEP > old;
+    const unsigned char *sl = ringp + slot * SLOTB;
+    f32x4 s[RT];
+    {
+      f32x4 part[RT][NQ];
+#pragma unroll
+      for (int j0 = 0; j0 < NQ; j0 += 4) {           // eight chains side by side
+        f32x4 k[4], z[RT][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const f32x4 *>(sl + l16 * ROWB + ((4 * (j0 + j) + q) ^ fK(l16)) * 16);
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int h = 0; h < 4; ++h)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const f32x4 x = __builtin_bit_cast(f32x4, qf[t][j0 + j]), none = {0.f, 0.f, 0.f, 0.f};
+              f32x4 &y = h & 1 ? z[t][j] : part[t][j0 + j];
+              y = __builtin_amdgcn_mfma_f32_16x16x4f32(k[j][h], x[h], h < 2 ? none : y, 0, 0, 0);
+            }
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) part[t][j0 + j] += z[t][j];
+      }
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+#pragma unroll
+        for (int w = NQ / 2; w >= 1; w /= 2)
+#pragma unroll
+          for (int j = 0; j < w; ++j) part[t][j] += part[t][j + w];
+        s[t] = part[t][0];
+      }
+    }
+    f32x4 vf[NH][4];                                 // [h][r]: dims 64h + 4 l16 + (0..3) of key 4q + r
+#pragma unroll
+    for (int h = 0; h < NH; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        vf[h][r] = *reinterpret_cast<const f32x4 *>(sl + HALFB + (4 * q + r) * ROWB + (16 * h + l16) * 16);
+    f32x4 kp;
+    if (BIAS) kp = *reinterpret_cast<const f32x4 *>(&s_pos[NS * ks + slot][4 * q]);
+    float p[RT][4];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const uint32_t see = (masked ? seen(t, t0) : ~0u) >> (4 * q);
+      float mx = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = BIAS ? fmaf(s[t][i], scale2, fmaf(rows.slope2[t], kp[i], rows.bias0[t])) : s[t][i] * scale2;
+        p[t][i] = see >> i & 1 ? x : -INFINITY;
+        mx = fmaxf(mx, p[t][i]);
+      }
+      if (__any(mx > m_run[t])) {                    // the reference is the maximum itself (see the fp32 prefill)
+        const float m_new = fmaxf(m_run[t], rows_max(mx)), alpha = fast_exp2(m_run[t] - m_new);
+        m_run[t] = m_new;
+        l_run[t] *= alpha;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) o[t][c] *= alpha;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[t][i] = fast_exp2(p[t][i] - m_run[t]);
+      l_run[t] += (p[t][0] + p[t][1]) + (p[t][2] + p[t][3]);
+    }
+    if (masked) {
+      bool bad = false;
+#pragma unroll
+      for (int h = 0; h < NH; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) bad |= not_finite(vf[h][r][e]);
+      if (__any(bad)) {
+        add_infinite(t0, [&](int t, int i) { return p[t][i]; }, [&](int c, int e) { return 64 * (c / 4) + 16 * q + 4 * e + c % 4; });
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (not_finite(vf[h][r][e])) vf[h][r][e] = 0.f;
+      }
+    }
+    // o[t][4h + c][r]: dim 64h + 16 q + 4r + c of the lane's row
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int h = 0; h < NH; ++h) {
+        f32x4 x[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) x[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) x[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[h][r][c], p[t][r], x[c], 0, 0, 0);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[t][4 * h + c] += x[c];
+      }
+  };
+  auto compute = [&](int step, int slot) {
+    if constexpr (kBf16) compute_bf16(step, slot);
+    else compute_f32(step, slot);
   };
 
   // RW waves: NS - 1 stages are on their way when a step begins; one wave: NS when it waits
@@ -509,7 +663,7 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void tree_bf16_kernel(PlanDev pd, 
     if constexpr (RW > 1) {
       __syncthreads();                             // this stage is there, and nobody reads the slot of the one before any more
       if (s + AHEAD * KS < n_steps) issue(s + AHEAD * KS, slot == 0 ? NS - 1 : slot - 1);
-      if (s < n_steps) compute(s, slot);
+      if (s < n_steps && row0 < n * G) compute(s, slot);      // a wave without rows only fetches
     } else {
       if (s < n_steps) compute(s, slot);
       // the reads of this slot have returned before the next stage may overwrite it
@@ -520,212 +674,19 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void tree_bf16_kernel(PlanDev pd, 
   }
 #pragma unroll
   for (int t = 0; t < RT; ++t) l_run[t] = rows_sum(l_run[t]);
-  finish<__bf16, D, RT, RW, KS>(pd, d, b, g, n, rows, m_run, l_run, o, reinterpret_cast<float *>(ring), [&](int c) { return 16 * c + 4 * q; });
-}
-
-// fp32 on v_mfma_f32_16x16x4_f32, 16 keys a step, everything in 32 bits; K and V come from memory straight into registers.
-//   S^T[key, row] = K[key, :] . Q[row, :]       slots bound to dims 16 i + 4 (L / 16) + e
-//   O^T[d, row]  += V^T[d, key] . P^T[key, row] slot L / 16 of step r bound to key 4 (L / 16) + r; rows of O^T to dims 64 h + 4 (L % 16) + c
-// Sums are kept in short chains that are added up (a single chain of D products rounds several times as much).
-template <int D, int RT, int KS, bool BIAS>
-__global__ __launch_bounds__(64 * KS, 2) void tree_f32_kernel(PlanDev pd, TreeDev d) {
-  constexpr int NI = D / 16, NH = D / 64;
-  __shared__ __attribute__((aligned(16))) float merge[KS > 1 ? (KS - 1) * RT * 16 * (D + 4) : 4];
-  __shared__ KeyTable tab;
-  const TreeArgs &a = d.a;
-  const int Hq = pd.n_q_heads, Hkv = pd.n_kv_heads, G = Hq / Hkv;
-  const int b = blockIdx.x / Hkv, g = blockIdx.x % Hkv;
-  const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const RespRows rr = resp_rows(a, b);
-  const int n = a.n_nodes ? min(max(a.n_nodes[b], 0), a.max_nodes) : a.max_nodes;
-  if (blockIdx.y == gridDim.y - 1) {
-    if (blockIdx.z == 0) append_nodes<float, D>(pd, a, b, g, rr.write, n);
-    return;
-  }
-  const int row0 = int(blockIdx.y) * 16 * RT;
-
-  Rows<RT> rows;
-  find_rows<RT, BIAS>(pd, a, b, g, row0, rows);
-  const int up = load_parent(a, b);
-  float qf[RT][4 * NI];
-  const float scale2 = a.scale * kLog2e;
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    const float *qp = static_cast<const float *>(a.q_new) + (((int64_t)b * a.max_nodes + rows.node[t]) * Hq + rows.head[t]) * D + 4 * q;
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const f32x4 v = *reinterpret_cast<const f32x4 *>(qp + 16 * i);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) qf[t][4 * i + e] = v[e] * scale2;
-    }
-  }
-  if (row0 >= n * G) return;
-  build_key_table<float, D>(pd, a, b, g, rr.read, NewKeys{b * a.max_nodes, n, int64_t(Hkv) * D * 4}, BIAS, tab);
-  const RangeSearch find(tab);
-  const int n_total = tab.n_total, old = n_total - n;
-  const int piece = ((n_total + d.n_pieces - 1) / d.n_pieces + 31) & ~31;
-  const int key0 = min(int(blockIdx.z) * piece, n_total), key1 = min(key0 + piece, n_total);
-
-  float m_run[RT], l_run[RT];
-  f32x4 o[RT][NI];                   // o[t][4h + c][r]: dim 64h + 16 q + 4r + c of the lane's row
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    m_run[t] = kNegBig;
-    l_run[t] = 0.f;
-#pragma unroll
-    for (int c = 0; c < NI; ++c) o[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-
-  struct Stage {
-    f32x4 k[NI], v[NH][4];
-    float pos[4];
-  };
-  auto load = [&](int t0, Stage &st) {
-    const int i0 = find.uniform(t0);
-    const int c0 = __builtin_amdgcn_readfirstlane(tab.cum[i0]), c1 = __builtin_amdgcn_readfirstlane(tab.cum[i0 + 1]);
-    const bool plain = t0 + 16 <= c1;
-    const int64_t stride = uniform64(tab.stride[i0]);
-    auto at = [&](int key, bool v) -> const char * {
-      if (plain) return (v ? tab.v[i0] : tab.k[i0]) + int64_t(key - c0) * stride;
-      const int vk = min(key, n_total - 1), i = find.from(i0, vk);
-      return (v ? tab.v[i] : tab.k[i]) + int64_t(vk - tab.cum[i]) * tab.stride[i];
-    };
-    const char *kp = at(t0 + l16, false) + 16 * q;
-#pragma unroll
-    for (int i = 0; i < NI; ++i) st.k[i] = *global_ptr<f32x4>(kp + 64 * i);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const char *vp = at(t0 + 4 * q + r, true) + 16 * l16;
-#pragma unroll
-      for (int h = 0; h < NH; ++h) st.v[h][r] = *global_ptr<f32x4>(vp + 256 * h);
-      if (BIAS) {
-        const int vk = min(t0 + 4 * q + r, n_total - 1), i = find.from(i0, vk);
-        st.pos[r] = global_ptr<float>(tab.pos[i])[vk - tab.cum[i]];
-      }
-    }
-  };
-  auto step = [&](int t0, Stage &st, auto masked) {
-    constexpr bool MASKED = decltype(masked)::value;
-    float p[RT][4];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      f32x4 s[NI];
-#pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
-        x = __builtin_amdgcn_mfma_f32_16x16x4f32(st.k[i][0], qf[t][4 * i], x, 0, 0, 0);
-        y = __builtin_amdgcn_mfma_f32_16x16x4f32(st.k[i][1], qf[t][4 * i + 1], y, 0, 0, 0);
-        x = __builtin_amdgcn_mfma_f32_16x16x4f32(st.k[i][2], qf[t][4 * i + 2], x, 0, 0, 0);
-        y = __builtin_amdgcn_mfma_f32_16x16x4f32(st.k[i][3], qf[t][4 * i + 3], y, 0, 0, 0);
-        s[i] = x + y;
-      }
-#pragma unroll
-      for (int w = NI / 2; w >= 1; w /= 2)
-#pragma unroll
-        for (int i = 0; i < w; ++i) s[i] += s[i + w];
-      float mx = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float x = s[0][i];
-        if (BIAS) x += fmaf(rows.slope2[t], st.pos[i], rows.bias0[t]);
-        if (MASKED) {
-          const int at = t0 + 4 * q + i - old;
-          if (at >= n || (at >= 0 && !(rows.mask[t] >> (at & 63) & 1))) x = -INFINITY;
-        }
-        p[t][i] = x;
-        mx = fmaxf(mx, x);
-      }
-      if (__any(mx > m_run[t])) {
-        const float m_new = fmaxf(m_run[t], rows_max(mx)), alpha = fast_exp2(m_run[t] - m_new);
-        m_run[t] = m_new;
-        l_run[t] *= alpha;
-#pragma unroll
-        for (int c = 0; c < NI; ++c) o[t][c] *= alpha;
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        p[t][i] = fast_exp2(p[t][i] - m_run[t]);
-        l_run[t] += p[t][i];
-      }
-    }
-    if (MASKED) {
-      bool bad = false;
-#pragma unroll
-      for (int h = 0; h < NH; ++h)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) bad |= not_finite(st.v[h][r][e]);
-      if (__any(bad)) {                            // as in the bf16 kernel
-        const int i0 = find.uniform(t0);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll 1
-          for (int from = 0; from < 4; ++from) {
-            const int vk = min(t0 + 4 * from + i, n_total - 1), r = find.from(i0, vk);
-            const float *v = reinterpret_cast<const float *>(tab.v[r] + int64_t(vk - tab.cum[r]) * tab.stride[r]);
-#pragma unroll
-            for (int t = 0; t < RT; ++t) {
-              const float w = __shfl(p[t][i], 16 * from + l16);
-#pragma unroll
-              for (int c = 0; c < NI; ++c)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const float x = v[64 * (c / 4) + 16 * q + 4 * e + c % 4];
-                  if (not_finite(x) && w != 0.f) o[t][c][e] += w * x;
-                }
-            }
-          }
-#pragma unroll
-        for (int h = 0; h < NH; ++h)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (not_finite(st.v[h][r][e])) st.v[h][r][e] = 0.f;
-      }
-    }
+  if constexpr (kBf16) {
+    finish<T, D, RT, RW, KS>(pd, d, b, g, n, rows, m_run, l_run, o, reinterpret_cast<float *>(ring), [&](int c) { return 16 * c + 4 * q; });
+  } else {
+    f32x4 ov[RT][NC];                // [4h + r]: four dims from 64h + 16 q + 4r on
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
-      for (int h = 0; h < NH; ++h)
+      for (int h = 0; h < NC / 4; ++h)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int r = 0; r < 4; ++r) x = __builtin_amdgcn_mfma_f32_16x16x4f32(st.v[h][r][c], p[t][r], x, 0, 0, 0);
-          o[t][4 * h + c] += x;
-        }
-  };
-  auto compute = [&](int t0, Stage &st) {
-    if (t0 + 16 > old) step(t0, st, std::true_type{});
-    else step(t0, st, std::false_type{});
-  };
-  // the loads of a step leave before the arithmetic of the one before
-  constexpr int STEP = 16 * KS;
-  Stage s0, s1;
-  int t0 = key0 + 16 * wave;
-  if (t0 < key1) load(t0, s0);
-  find_masks(pd, n, up, row0, rows);
-  while (t0 < key1) {
-    if (t0 + STEP < key1) load(t0 + STEP, s1);
-    compute(t0, s0);
-    t0 += STEP;
-    if (t0 >= key1) break;
-    if (t0 + STEP < key1) load(t0 + STEP, s0);
-    compute(t0, s1);
-    t0 += STEP;
+        for (int r = 0; r < 4; ++r) ov[t][4 * h + r] = f32x4{o[t][4 * h][r], o[t][4 * h + 1][r], o[t][4 * h + 2][r], o[t][4 * h + 3][r]};
+    finish<T, D, RT, RW, KS>(pd, d, b, g, n, rows, m_run, l_run, ov, reinterpret_cast<float *>(ring),
+                             [&](int i) { return 64 * (i / 4) + 16 * q + 4 * (i % 4); });
   }
-#pragma unroll
-  for (int t = 0; t < RT; ++t) l_run[t] = rows_sum(l_run[t]);
-  f32x4 ov[RT][NI];                  // [4h + r]: four dims from 64h + 16 q + 4r on
-#pragma unroll
-  for (int t = 0; t < RT; ++t)
-#pragma unroll
-    for (int h = 0; h < NH; ++h)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) ov[t][4 * h + r] = f32x4{o[t][4 * h][r], o[t][4 * h + 1][r], o[t][4 * h + 2][r], o[t][4 * h + 3][r]};
-  finish<float, D, RT, 1, KS>(pd, d, b, g, n, rows, m_run, l_run, ov, merge, [&](int i) { return 64 * (i / 4) + 16 * q + 4 * (i % 4); });
 }
 
 // How a launch is shared out, a function of the call's sizes alone.  Measured, bf16, 128 dims, us for one layer (~500 keys, 32 KV
@@ -737,7 +698,10 @@ __global__ __launch_bounds__(64 * KS, 2) void tree_f32_kernel(PlanDev pd, TreeDe
 //     4 row waves 39 / 39 / 41 / 60
 // Hence: as many key groups as leave a workgroup to every compute unit (their slots fill its LDS), none where there are more
 // workgroups than that; four waves to share a stage once two would give more workgroups than compute units.
-// Lists are cut into pieces of at least a step for every key group where that still leaves compute units without a workgroup.
+//   fp32, 48 pairs of 890 keys, up to 48 / 192 rows: 1 row wave times 4 key groups 45 / 125, in 2 pieces 33 / 139; 4 row waves 116 / 122,
+//     in 5 pieces 52 / 79.  512 / 1024 pairs, up to 16 rows: 1 wave 128 / 168, 2 key groups 83 / 166, 4 87 / 177
+// Lists are cut into pieces, of at least a step for every key group, where that leaves compute units without a workgroup (fp32
+// with four row waves, of which three workgroups are resident: without three).
 struct TreeShape {
   int rt, rw, ks, blocks, pieces;
 };
@@ -757,11 +721,13 @@ static TreeShape tree_shape(const sp_plan *plan, int max_nodes, int64_t keys, in
     else if (n <= 2 * n_cu && t.rw == 1) t.ks = 2;
   } else {
     t.rt = 1;
-    t.ks = 4;
+    if (rows > 64) t.rw = 4;
+    else t.ks = wgs() <= 2 * n_cu ? 4 : 2;
   }
   const int64_t n = wgs();
   if (n <= kTreeCounters) {
-    int64_t p = std::min<int64_t>(n_cu / n, (keys + 16 * t.ks) / (32 * t.ks));
+    int64_t p = ((plan->dtype == SP_F32 && t.rw == 4 ? 3 : 1) * n_cu + n / 2) / n;
+    p = std::min<int64_t>(p, (keys + 16 * t.ks) / (32 * t.ks));
     p = std::min<int64_t>(p, int64_t(kTreePartBytes) / (part_rows * (plan->head_dim + 2) * 4));
     t.pieces = int(std::max<int64_t>(p, 1));
   }
@@ -775,13 +741,14 @@ static hipError_t launch_tree(const sp_plan *plan, TreeDev &d, const TreeShape &
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, plan->dev, d); };
   auto pick = [&](auto bias) {
     constexpr bool BIAS = decltype(bias)::value;
-    if constexpr (sizeof(T) == 4) go(tree_f32_kernel<D, 1, 4, BIAS>);
-    else if (t.rw == 4) t.ks == 2 ? go(tree_bf16_kernel<D, 2, 4, 2, 4, BIAS>) : go(tree_bf16_kernel<D, 2, 4, 1, 3, BIAS>);
-    else if (t.rw == 2) t.ks == 4 ? go(tree_bf16_kernel<D, 2, 2, 4, 2, BIAS>) : go(tree_bf16_kernel<D, 2, 2, 1, 2, BIAS>);
-    else if (t.rt == 1) t.ks == 4 ? go(tree_bf16_kernel<D, 1, 1, 4, 2, BIAS>) : t.ks == 2 ? go(tree_bf16_kernel<D, 1, 1, 2, 2, BIAS>)
-                                                                                          : go(tree_bf16_kernel<D, 1, 1, 1, 2, BIAS>);
-    else t.ks == 4 ? go(tree_bf16_kernel<D, 2, 1, 4, 2, BIAS>) : t.ks == 2 ? go(tree_bf16_kernel<D, 2, 1, 2, 2, BIAS>)
-                                                                           : go(tree_bf16_kernel<D, 2, 1, 1, 2, BIAS>);
+    if constexpr (sizeof(T) == 4) t.rw == 4 ? go(tree_kernel<T, D, 1, 4, 1, 3, BIAS>) : t.ks == 4 ? go(tree_kernel<T, D, 1, 1, 4, 2, BIAS>)
+                                                                                                 : go(tree_kernel<T, D, 1, 1, 2, 2, BIAS>);
+    else if (t.rw == 4) t.ks == 2 ? go(tree_kernel<T, D, 2, 4, 2, 4, BIAS>) : go(tree_kernel<T, D, 2, 4, 1, 3, BIAS>);
+    else if (t.rw == 2) t.ks == 4 ? go(tree_kernel<T, D, 2, 2, 4, 2, BIAS>) : go(tree_kernel<T, D, 2, 2, 1, 2, BIAS>);
+    else if (t.rt == 1) t.ks == 4 ? go(tree_kernel<T, D, 1, 1, 4, 2, BIAS>) : t.ks == 2 ? go(tree_kernel<T, D, 1, 1, 2, 2, BIAS>)
+                                                                                          : go(tree_kernel<T, D, 1, 1, 1, 2, BIAS>);
+    else t.ks == 4 ? go(tree_kernel<T, D, 2, 1, 4, 2, BIAS>) : t.ks == 2 ? go(tree_kernel<T, D, 2, 1, 2, 2, BIAS>)
+                                                                           : go(tree_kernel<T, D, 2, 1, 1, 2, BIAS>);
   };
   if (plan->has_slopes) pick(std::true_type{}); else pick(std::false_type{});
   return hipGetLastError();
