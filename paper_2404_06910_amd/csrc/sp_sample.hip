@@ -11,7 +11,9 @@
 // the order of the additions (equal calls give equal tokens), and a weight is off by at most 2^-(62 - bits of the vocabulary), 2^-45 of
 // the largest at 128256 tokens.  Tokens lighter than that cannot be drawn.
 //
-// One workgroup per row.
+// One workgroup per row.  bf16 rows take counts alone: there are 65536 values, so a histogram of all of them in LDS is the sorted row, and a
+// weight is computed once per value that occurs, not per token (sample_counts).  fp32, and the bf16 rows that the 16-bit counts cannot
+// hold, build histograms of weights over the first 13 bits and go on inside a bin (RowSearch).
 #include "sp_device.h"
 #include "sp_internal.h"
 
@@ -22,7 +24,7 @@ namespace {
 constexpr int kSampleThreads = 1024;
 constexpr int kSampleWaves = kSampleThreads / 64;
 constexpr int kBinBits = 13, kBins = 1 << kBinBits;
-constexpr int kList = 4096;                     // keys of one bin that are searched in LDS
+constexpr int kList = 2048;                     // keys of one bin that are searched in LDS
 constexpr uint32_t kNegInfKey = 0x007fffffu;    // value_key(-inf)
 
 // Order of a value as an unsigned number (the larger the earlier); -0 counts as +0.
@@ -48,52 +50,97 @@ struct SampleLds {
   uint32_t dcount[256];
   u64 wave_mass[kSampleWaves], wave_top[kSampleWaves];
   uint32_t wave_count[kSampleWaves];
+  double table[64];
   Place place;
-  uint32_t n_list, found_key, found_index;
+  uint32_t n_list, n_kept, found_key, found_index;
+  u64 kept[kList];                              // the tokens that top-k leaves, and those with equal first bits
 };
 
+// exp(.) by a table of 2^(i/64) in LDS and a polynomial for what is left, |r| <= ln 2 / 128 (table-driven reduction; the sixth-order rest
+// is below 4e-17): about half the instructions of the library's.
 struct Weights {
   float m;          // largest logit
-  double inv_t, scale;
+  double inv_t;     // log2 e * 64 / temperature
+  int s_bits;       // weights are multiples of 2^-s_bits
+  const double *table;
   __device__ __forceinline__ u64 operator()(float x) const {
-    if (x == m) return u64(scale);
-    if (m == INFINITY) return 0;
-    return u64(exp((double(x) - double(m)) * inv_t) * scale);
+    if (x == m) return u64(1) << s_bits;
+    const double z = (double(x) - double(m)) * inv_t;            // in 64ths of an octave
+    if (!(z > -64.0 * 64.0) || m == INFINITY) return 0;          // below 2^-64
+    const double n = rint(z), r = (z - n) * (0.69314718055994530942 / 64.0);
+    const int i = int(n);
+    double p = fma(r, 1.0 / 120.0, 1.0 / 24.0);
+    p = fma(p, r, 1.0 / 6.0);
+    p = fma(p, r, 0.5);
+    p = fma(p * r, r, r);
+    const double t = table[i & 63];
+    return u64(ldexp(fma(t, p, t), (i >> 6) + s_bits));
   }
 };
+// the table; threads below 64
+__device__ __forceinline__ void fill_table(double *table) {
+  if (threadIdx.x < 64) table[threadIdx.x] = exp2(double(threadIdx.x) / 64.0);
+}
 
 // fn(x, index) for every element of a row, in no order
 template <typename T, class F>
 __device__ __forceinline__ void for_row(const T *row, int vocab, F &&fn) {
-  constexpr int EV = Elem<T>::kVec;
+  constexpr int EV = Elem<T>::kVec, U = 4;       // loads in flight
   const int n_vec = vocab / EV;
-  for (int v = threadIdx.x; v < n_vec; v += kSampleThreads) {
-    float x[EV];
-    Elem<T>::unpack(ld16(row + int64_t(v) * EV), x);
+  for (int v0 = threadIdx.x; v0 < n_vec; v0 += U * kSampleThreads) {
+    u32x4 raw[U];
 #pragma unroll
-    for (int e = 0; e < EV; ++e) fn(x[e], v * EV + e);
+    for (int u = 0; u < U; ++u) raw[u] = ld16(row + int64_t(min(v0 + u * kSampleThreads, n_vec - 1)) * EV);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int v = v0 + u * kSampleThreads;
+      if (v >= n_vec) break;
+      float x[EV];
+      Elem<T>::unpack(raw[u], x);
+#pragma unroll
+      for (int e = 0; e < EV; ++e) fn(x[e], v * EV + e);
+    }
   }
   const int i = n_vec * EV + threadIdx.x;
   if (i < vocab) fn(Elem<T>::load1(row + i), i);
 }
 
+// x of the lane that the DPP control names, 0 where it names none (or the row mask leaves the row out)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 dpp(u64 x) { return u64(dpp<CTRL, ROWS>(uint32_t(x >> 32))) << 32 | dpp<CTRL, ROWS>(uint32_t(x)); }
+// Sum over the lanes up to this one: in the rows of 16 by shifts, then the last lanes of rows to the rows behind.  (Through LDS, by
+// shuffles, a scan of weights and counts takes three times as long, and a row is a chain of them.)
+template <class X>
+__device__ __forceinline__ X wave_scan(X x) {
+  x += dpp<0x111, 0xf>(x);                       // row_shr 1, 2, 4, 8
+  x += dpp<0x112, 0xf>(x);
+  x += dpp<0x114, 0xf>(x);
+  x += dpp<0x118, 0xf>(x);
+  x += dpp<0x142, 0xa>(x);                       // row_bcast 15, 31
+  x += dpp<0x143, 0xc>(x);
+  return x;
+}
+__device__ __forceinline__ u64 lane_value(u64 x, int lane) {
+  return u64(uint32_t(__builtin_amdgcn_readlane(uint32_t(x >> 32), lane))) << 32 | uint32_t(__builtin_amdgcn_readlane(uint32_t(x), lane));
+}
+__device__ __forceinline__ uint32_t lane_value(uint32_t x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+
 // sums over the threads before this one
-__device__ __forceinline__ void scan_before(SampleLds &s, u64 &mass, uint32_t &count) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const u64 own_mass = mass;
-  const uint32_t own_count = count;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const u64 m = __shfl_up(mass, off);
-    const uint32_t c = __shfl_up(count, off);
-    if (lane >= off) { mass += m; count += c; }
-  }
+template <class Lds>
+__device__ __forceinline__ void scan_before(Lds &s, u64 &mass, uint32_t &count) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const u64 m = wave_scan(mass);
+  const uint32_t c = wave_scan(count);
   __syncthreads();
-  if (lane == 63) { s.wave_mass[wave] = mass; s.wave_count[wave] = count; }
+  if (lane == 63) { s.wave_mass[wave] = m; s.wave_count[wave] = c; }
   __syncthreads();
-  mass -= own_mass;
-  count -= own_count;
-  for (int w = 0; w < wave; ++w) { mass += s.wave_mass[w]; count += s.wave_count[w]; }
+  // the waves' sums are scanned by the lanes below 16 of every wave
+  const u64 wm = wave_scan(lane < kSampleWaves ? s.wave_mass[lane & (kSampleWaves - 1)] : 0);
+  const uint32_t wc = wave_scan(lane < kSampleWaves ? s.wave_count[lane & (kSampleWaves - 1)] : 0);
+  mass = m - mass + (wave ? lane_value(wm, wave - 1) : 0);
+  count = c - count + (wave ? lane_value(wc, wave - 1) : 0);
 }
 
 // The bin, from the highest down, at which the running weight (or count) reaches target.
@@ -133,19 +180,30 @@ struct RowSearch {
   uint32_t least;        // value keys below it take no part
   Weights weight;
   SampleLds &s;
+  bool few = false;      // what takes part is in s.kept
+
+  template <class F>
+  __device__ __forceinline__ void each(F &&fn) const {
+    if (few) {
+      for (uint32_t i = threadIdx.x; i < s.n_kept; i += kSampleThreads) fn(key_value(uint32_t(s.kept[i] >> 32)), int(~uint32_t(s.kept[i])));
+    } else {
+      for_row(row, vocab, fn);
+    }
+  }
 
   __device__ __forceinline__ bool in(float x, uint32_t k) const { return x == x && k >= least; }
 
   // histogram over the `bits` bits of the value key above `shift`, of the keys that begin with prefix
+  template <bool MASS = true>
   __device__ __forceinline__ void histogram(int shift, int bits, uint32_t prefix) {
     __syncthreads();
     for (int i = threadIdx.x; i < kBins; i += kSampleThreads) { s.mass[i] = 0; s.count[i] = 0; }
     __syncthreads();
-    for_row(row, vocab, [&](float x, int) {
+    each([&](float x, int) {
       const uint32_t k = value_key(x);
       if (!in(x, k) || (shift + bits < 32 && (k >> (shift + bits)) != prefix)) return;
       const uint32_t b = (k >> shift) & ((1u << bits) - 1);
-      atomicAdd(&s.mass[b], weight(x));
+      if (MASS) atomicAdd(&s.mass[b], weight(x));
       atomicAdd(&s.count[b], 1u);
     });
     __syncthreads();
@@ -215,7 +273,7 @@ struct RowSearch {
       __syncthreads();
       if (threadIdx.x == 0) s.n_list = 0;
       __syncthreads();
-      for_row(row, vocab, [&](float x, int i) {
+      each([&](float x, int i) {
         const uint32_t k = value_key(x);
         if (in(x, k) && (k >> shift) == prefix) s.list[atomicAdd(&s.n_list, 1u)] = (u64(k) << 32) | uint32_t(~i);
       });
@@ -262,16 +320,48 @@ struct RowSearch {
   }
 };
 
-template <typename T>
-__global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
-  __shared__ SampleLds s;
-  const int64_t r = blockIdx.x;
+// The settings of a row.
+struct Settings {
+  float temperature, top_p, min_p, u;
+  int32_t top_k;
+};
+__device__ __forceinline__ Settings settings_of(const SampleArgs &a, int64_t r) {
   const int64_t set = r / a.rows_per_set;
+  return {a.temperature ? a.temperature[set] : 1.f, a.top_p ? a.top_p[set] : 1.f, a.min_p ? a.min_p[set] : 0.f,
+          fminf(fmaxf(a.u[r], 0.f), 0x1.fffffep-1f), a.top_k ? a.top_k[set] : 0};      // u: NaN counts as 0
+}
+__device__ __forceinline__ Weights weights_of(float m, float temperature, int vocab, const double *table) {
+  return Weights{m, 64.0 * 1.44269504088896340736 / double(temperature), 62 - (32 - __clz((vocab - 1) | 1)), table};
+}
+// least value that min-p leaves
+__device__ __forceinline__ float min_p_value(float m, float temperature, float min_p) {
+  if (!(min_p > 0.f)) return -INFINITY;
+  if (min_p >= 1.f) return m;
+  const double limit = double(m) + double(temperature) * log(double(min_p));
+  const float f = float(limit);
+  return double(f) < limit ? nextafterf(f, INFINITY) : f;
+}
+// what top-p leaves of a total weight begins at the token that reaches this; the draw is the token that reaches that
+__device__ __forceinline__ u64 top_p_target(float top_p, u64 total) {
+  const double want = ceil(double(fmaxf(top_p, 0.f)) * double(total));
+  return want < 1.0 ? 1 : min(u64(want), total);
+}
+__device__ __forceinline__ u64 draw_target(float u, u64 total) { return min(u64(floor(double(u) * double(total))) + 1, total); }
+__device__ __forceinline__ void write_result(const SampleArgs &a, int64_t r, int32_t token, float x, const Weights &w, float temperature,
+                                             u64 total) {
+  a.token[r] = token;
+  if (a.logprob) {
+    const double z = x == w.m ? 0.0 : (double(x) - double(w.m)) / double(temperature);
+    a.logprob[r] = float(z - log(ldexp(double(total), -w.s_bits)));
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void sample_general(const SampleArgs &a, int64_t r, SampleLds &s) {
   const T *row = static_cast<const T *>(a.logits) + r * a.row_stride;
   const int vocab = int(a.vocab);
-  const float temperature = a.temperature ? a.temperature[set] : 1.f;
-  const int32_t top_k = a.top_k ? a.top_k[set] : 0;
-  const float top_p = a.top_p ? a.top_p[set] : 1.f, min_p = a.min_p ? a.min_p[set] : 0.f;
+  const Settings set = settings_of(a, r);
+  fill_table(s.table);
 
   // the first token of the order
   u64 top = 0;
@@ -284,7 +374,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
   if ((threadIdx.x & 63) == 0) s.wave_top[threadIdx.x >> 6] = top;
   __syncthreads();
   for (int w = 0; w < kSampleWaves; ++w) top = s.wave_top[w] > top ? s.wave_top[w] : top;
-  if (top == 0 || !(temperature > 0.f)) {
+  if (top == 0 || !(set.temperature > 0.f)) {
     if (threadIdx.x == 0) {
       a.token[r] = top ? int32_t(~uint32_t(top)) : -1;
       if (a.logprob) a.logprob[r] = top ? 0.f : -INFINITY;
@@ -292,51 +382,351 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
     return;
   }
   const float m = key_value(uint32_t(top >> 32));
-  const int s_bits = 62 - (32 - __clz(vocab - 1 | 1));
-  RowSearch<T> find{row, vocab, kNegInfKey + 1, Weights{m, 1.0 / double(temperature), ldexp(1.0, s_bits)}, s};
-  if (min_p > 0.f) {
-    const double limit = min_p >= 1.f ? double(m) : double(m) + double(temperature) * log(double(min_p));
-    float f = float(limit);
-    if (double(f) < limit) f = nextafterf(f, INFINITY);
-    find.least = max(find.least, value_key(f));
-  }
-  find.histogram(32 - kBinBits, kBinBits, 0);
+  const uint32_t least = max(kNegInfKey + 1, value_key(min_p_value(m, set.temperature, set.min_p)));
+  RowSearch<T> find{row, vocab, least, weights_of(m, set.temperature, vocab, s.table), s};
   // what takes part in all
-  u64 total = 0;
-  uint32_t n = 0;
-  for (int i = threadIdx.x; i < kBins; i += kSampleThreads) { total += s.mass[i]; n += s.count[i]; }
-  {
-    const u64 own = total;
+  auto totals = [&](u64 &mass, uint32_t &n) {
+    mass = 0;
+    n = 0;
+    for (int i = threadIdx.x; i < kBins; i += kSampleThreads) { mass += s.mass[i]; n += s.count[i]; }
+    const u64 own = mass;
     const uint32_t own_n = n;
-    scan_before(s, total, n);
-    total += own;
-    n += own_n;
-    if (threadIdx.x == kSampleThreads - 1) s.place = Place{0, total, 0, n, 0};
+    scan_before(s, mass, n);
+    if (threadIdx.x == kSampleThreads - 1) s.place = Place{0, mass + own, 0, n + own_n, 0};
     __syncthreads();
-    total = s.place.mass;
+    mass = s.place.mass;
     n = s.place.count;
     __syncthreads();
-  }
-  if (top_k > 0 && uint32_t(top_k) < n) {
-    const Place p = find.select(u64(top_k), false, true);
-    total = p.mass_before + find.weight(key_value(s.found_key));
-  }
-  if (top_p < 1.f) {
-    const double want = ceil(double(fmaxf(top_p, 0.f)) * double(total));
-    const u64 target = want < 1.0 ? 1 : min(u64(want), total);
-    const Place p = find.select(target, true, true);
-    total = p.mass_before + find.weight(key_value(s.found_key));
-  }
-  const float u = fminf(fmaxf(a.u[r], 0.f), 0x1.fffffep-1f);      // NaN: 0
-  const u64 target = min(u64(floor(double(u) * double(total))) + 1, total);
-  find.select(target, true, false);
-  if (threadIdx.x == 0) {
-    a.token[r] = int32_t(s.found_index);
-    if (a.logprob) {
-      const float x = key_value(s.found_key);
-      const double z = x == m ? 0.0 : (double(x) - double(m)) * find.weight.inv_t;
-      a.logprob[r] = float(z - log(double(total) / find.weight.scale));
+  };
+  constexpr int kShift = 32 - kBinBits;
+  u64 total = 0;
+  uint32_t n = 0;
+  bool cut = false;
+  if (set.top_k > 0) {
+    // Counts tell which bins the first top_k tokens lie in.  The tokens of those bins (and no others) are weighed, and where they
+    // are few they are put aside, so that nothing below reads the row again.
+    find.template histogram<false>(kShift, kBinBits, 0);
+    totals(total, n);
+    cut = uint32_t(set.top_k) < n;
+    if (cut) {
+      reset_place(s);
+      const Place p = find_bin(s, s.mass, s.count, kBins, u64(set.top_k), false);
+      find.least = max(find.least, p.bin << kShift);
+      if (p.count_before + p.count <= kList) {
+        __syncthreads();
+        if (threadIdx.x == 0) s.n_kept = 0;
+        __syncthreads();
+        for_row(row, vocab, [&](float x, int i) {
+          const uint32_t k = value_key(x);
+          if (find.in(x, k)) s.kept[atomicAdd(&s.n_kept, 1u)] = (u64(k) << 32) | uint32_t(~i);
+        });
+        __syncthreads();
+        find.few = true;
+      }
     }
+  }
+  find.histogram(kShift, kBinBits, 0);
+  if (cut) {
+    const Place p = find.select(u64(set.top_k), false, true);
+    total = p.mass_before + find.weight(key_value(s.found_key));
+  } else {
+    totals(total, n);
+  }
+  if (set.top_p < 1.f) {
+    const Place p = find.select(top_p_target(set.top_p, total), true, true);
+    total = p.mass_before + find.weight(key_value(s.found_key));
+  }
+  find.select(draw_target(set.u, total), true, false);
+  if (threadIdx.x == 0) write_result(a, r, int32_t(s.found_index), key_value(s.found_key), find.weight, set.temperature, total);
+}
+
+__global__ __launch_bounds__(kSampleThreads) void sample_f32_kernel(SampleArgs a) {
+  __shared__ SampleLds s;
+  sample_general<float>(a, blockIdx.x, s);
+}
+__global__ __launch_bounds__(kSampleThreads) void sample_bf16_long_kernel(SampleArgs a) {
+  __shared__ SampleLds s;
+  sample_general<__bf16>(a, blockIdx.x, s);
+}
+
+// ---- bf16: a row as a histogram of its values ---------------------------------------------------------------------------
+
+// 16-bit order of a bf16 value: like value_key, but -0 comes right behind +0 (they weigh the same; only the search for a token's
+// index has to take them together).  Keys up to 0x7f are -inf and negative NaN, above 0xff80 (+inf) positive NaN.
+constexpr uint32_t kFirst16 = 0x80, kLast16 = 0xff80, kZero16 = 0x8000, kMinusZero16 = 0x7fff;
+__device__ __forceinline__ float key16_value(uint32_t k) { return __uint_as_float((k >> 15 ? k & 0x7fffu : ~k & 0xffffu) << 16); }
+
+struct CountLds {
+  uint32_t hist[1 << 15];               // two 16-bit counts each
+  u64 g_mass[1024];                     // of 64 keys: weight and number of the tokens that take part
+  uint32_t g_count[1024];
+  u64 flags[128];                       // a byte per group: has it any token?
+  u64 some[kSampleWaves];               // a bit per group
+  u64 wave_mass[kSampleWaves];
+  uint32_t wave_count[kSampleWaves];
+  double table[64];
+  u64 f_mass, total;
+  uint32_t f_group, f_count, n, counted, index, hits[16], wave_hits[kSampleWaves];
+};
+
+// A row of at most 8192 NV logits, NV vectors per thread, which stay in registers if there is room for them (KEEP) and are read
+// again, from the caches, when the token's index is looked for if not.  Returns false, having written nothing, if a value occurs too
+// often for a 16-bit count.
+template <int NV, bool KEEP>
+__device__ __forceinline__ bool sample_counts(const SampleArgs &a, int64_t r, CountLds &s) {
+  static_assert(KEEP || NV % 4 == 0, "read in fours");
+  constexpr uint32_t kPad = 0xff80ff80u;          // -inf
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int vocab = int(a.vocab), n_vec = (vocab + 7) / 8;
+  const uint16_t *row = static_cast<const uint16_t *>(a.logits) + r * a.row_stride;
+  auto load = [&](int i) {
+    const int at = i * kSampleThreads + tid;
+    u32x4 x = {kPad, kPad, kPad, kPad};
+    if (at < vocab / 8) x = ld16(row + int64_t(at) * 8);
+    return x;
+  };
+  u32x4 tail = {kPad, kPad, kPad, kPad};          // the last, partial vector, in place of the padding that its thread has there
+  const int tail_i = vocab % 8 && tid == vocab / 8 % kSampleThreads ? vocab / 8 / kSampleThreads : -1;
+  if (tail_i >= 0) {
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+      if (e < vocab % 8) {
+        const uint32_t x = row[vocab / 8 * 8 + e];
+        tail[e / 2] = e & 1 ? (tail[e / 2] & 0xffffu) | x << 16 : (tail[e / 2] & 0xffff0000u) | x;
+      }
+  }
+  u32x4 v[KEEP ? NV : 1];
+  if constexpr (KEEP)
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] = load(i);
+  const Settings set = settings_of(a, r);
+  fill_table(s.table);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) reinterpret_cast<u32x4 *>(s.hist)[i * kSampleThreads + tid] = u32x4{0, 0, 0, 0};
+  s.g_mass[tid] = 0;
+  s.g_count[tid] = 0;
+  if (tid < 16) s.hits[tid] = 0;
+  if (tid == 0) s.counted = 0;
+  __syncthreads();
+
+  // two keys of a word at once: all bits of a negative number flip, the sign of a positive one
+  auto keys = [](uint32_t w) { const uint32_t sign = (w >> 15) & 0x00010001u; return w ^ ((sign << 16) - sign | 0x80008000u); };
+  uint32_t out = 0;                               // -inf, counted by themselves: their 16 bits may overflow
+  const bool may_overflow = NV > 7 && n_vec * 8 > 65535;
+  // fn(vector, i) for all vectors of the thread; read from memory, four in flight
+  auto vectors = [&](auto &&fn) {
+    if constexpr (KEEP) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        fn(i == tail_i ? tail : v[i], i);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+#pragma unroll 1
+      for (int i0 = 0; i0 < NV; i0 += 4) {
+        u32x4 x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = load(i0 + j);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) fn(i0 + j == tail_i ? tail : x[j], i0 + j);
+      }
+    }
+  };
+  vectors([&](const u32x4 &x, int) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t k = keys(x[e]), lo = k & 0xffffu, hi = k >> 16;
+      if (may_overflow) out += (lo == 0x7f) + (hi == 0x7f);
+      atomicAdd(&s.hist[lo >> 1], (lo & 1) * 0xffffu + 1);
+      atomicAdd(&s.hist[hi >> 1], (hi & 1) * 0xffffu + 1);
+    }
+  });
+  __syncthreads();
+
+  // which groups of 64 keys hold any token: a wave reads 8 groups at a time, eight lanes a group
+  uint32_t counted = out;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int w0 = wave * 2048 + j * 256 + lane * 4;
+    u32x4 c = *reinterpret_cast<const u32x4 *>(&s.hist[w0]);
+    if (w0 == 0x7f / 2 / 4 * 4) c[0x7f / 2 % 4] &= 0xffffu;          // without -inf
+    const u64 some = __ballot((c[0] | c[1] | c[2] | c[3]) != 0);
+    if (lane == 0) s.flags[wave * 8 + j] = some;
+    if (may_overflow)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) counted += (c[e] & 0xffffu) + (c[e] >> 16);
+  }
+  if (may_overflow) {
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) counted += __shfl_xor(counted, off);
+    if (lane == 0) atomicAdd(&s.counted, counted);
+  }
+  __syncthreads();
+  // (a count that overflows loses 65536, or loses it and adds one to its neighbour)
+  if (may_overflow && s.counted != uint32_t(NV * kSampleThreads * 8)) return false;
+  {
+    const bool some = (s.flags[tid >> 3] >> (8 * (tid & 7)) & 0xff) != 0 && tid >= int(kFirst16 / 64) && tid <= int(kLast16 / 64);
+    const u64 b = __ballot(some);
+    if (lane == 0) s.some[wave] = b;
+  }
+  __syncthreads();
+  auto count_of = [&](uint32_t key) { return (s.hist[key >> 1] >> (16 * (key & 1))) & 0xffffu; };
+  // the largest value
+  uint32_t top = 0;
+  for (int w = kSampleWaves - 1; w >= 0 && top == 0; --w) {
+    u64 b = s.some[w];
+    while (b && top == 0) {
+      const int g = 63 - __builtin_clzll(b);
+      b &= ~(u64(1) << g);
+      const uint32_t key = uint32_t(w * 64 + g) * 64 + lane;
+      const u64 here = __ballot(key <= kLast16 && count_of(key) > 0);
+      if (here) top = uint32_t(w * 64 + g) * 64 + (63 - __builtin_clzll(here));
+    }
+  }
+  const float m = key16_value(top);
+
+  // the n-th (from 0) token with this key, by index; `several`: there are more
+  auto index_of = [&](uint32_t key, uint32_t n, bool several) {
+    const uint32_t raw = key >> 15 ? key & 0x7fffu : ~key & 0xffffu, pair = raw | raw << 16;
+    const uint32_t mask = raw << 17 ? ~0u : 0x7fff7fffu;              // zeros of both signs
+    auto hits = [&](const u32x4 &x) {
+      uint32_t h = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t d = (x[e] ^ pair) & mask;
+        h |= uint32_t((d & 0xffffu) == 0) << (2 * e) | uint32_t((d >> 16) == 0) << (2 * e + 1);
+      }
+      return h;
+    };
+    vectors([&](const u32x4 &x, int i) {
+      if (const uint32_t h = hits(x)) {
+        if (several) atomicAdd(&s.hits[i], uint32_t(__popc(h)));
+        else s.index = uint32_t(i * kSampleThreads + tid) * 8 + __ffs(h) - 1;
+      }
+    });
+    __syncthreads();
+    if (several) {
+      int i = 0;
+      while (i < NV - 1 && n >= s.hits[i]) n -= s.hits[i++];
+      u32x4 x = {kPad, kPad, kPad, kPad};
+      if constexpr (KEEP) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) x = i == j ? v[j] : x;
+      } else {
+        x = load(i);
+      }
+      const uint32_t h = hits(i == tail_i ? tail : x);
+      uint32_t before = wave_scan(uint32_t(__popc(h)));
+      if (lane == 63) s.wave_hits[wave] = before;
+      __syncthreads();
+      before -= __popc(h);
+      for (int w = 0; w < wave; ++w) before += s.wave_hits[w];
+      if (before <= n && n < before + __popc(h)) {
+        uint32_t left = h;
+        for (; before < n; ++before) left &= left - 1;
+        s.index = uint32_t(i * kSampleThreads + tid) * 8 + __ffs(left) - 1;
+      }
+      __syncthreads();
+    }
+    return int32_t(s.index);
+  };
+
+  if (top == 0 || !(set.temperature > 0.f)) {
+    const bool zero = top == kZero16 || top == kMinusZero16;
+    const int32_t token = top ? index_of(top, 0, zero ? count_of(kZero16) + count_of(kMinusZero16) > 1 : count_of(top) > 1) : -1;
+    if (tid == 0) {
+      a.token[r] = token;
+      if (a.logprob) a.logprob[r] = top ? 0.f : -INFINITY;
+    }
+    return true;
+  }
+  const Weights weight = weights_of(m, set.temperature, vocab, s.table);
+  const float least = min_p_value(m, set.temperature, set.min_p);
+
+  // weigh the groups that hold any: wave w takes every 16th
+  for (int b = 0; b < kSampleWaves; ++b) {
+    u64 mine = s.some[b] & (0x0001000100010001ull << wave);
+    while (mine) {
+      const int g = b * 64 + __builtin_ctzll(mine);
+      mine &= mine - 1;
+      const uint32_t key = uint32_t(g) * 64 + lane;
+      const float x = key16_value(key);
+      uint32_t c = key <= kLast16 && x >= least ? count_of(key) : 0;
+      u64 mass = c ? c * weight(x) : 0;
+      mass = wave_scan(mass);
+      c = wave_scan(c);
+      if (lane == 63) { s.g_mass[g] = mass; s.g_count[g] = c; }
+    }
+  }
+  __syncthreads();
+  // thread t has the group that is t-th from the top
+  const u64 g_mass = s.g_mass[1023 - tid];
+  const uint32_t g_count = s.g_count[1023 - tid];
+  u64 mass_before = g_mass;
+  uint32_t count_before = g_count;
+  scan_before(s, mass_before, count_before);
+  if (tid == kSampleThreads - 1) { s.total = mass_before + g_mass; s.n = count_before + g_count; }
+  __syncthreads();
+
+  struct Found {
+    uint32_t key, count, nth;             // the value, its tokens, and which of them
+    u64 mass;                             // of the order up to that token
+  };
+  auto find = [&](u64 target, bool by_mass) {
+    if (by_mass ? mass_before < target && target <= mass_before + g_mass
+                : count_before < target && target <= u64(count_before) + g_count) {
+      s.f_group = 1023 - tid;
+      s.f_mass = mass_before;
+      s.f_count = count_before;
+    }
+    __syncthreads();
+    // every wave for itself: lane L has key 63 - L of the group
+    const uint32_t key = s.f_group * 64 + 63 - lane;
+    const float x = key16_value(key);
+    const uint32_t c = key <= kLast16 && x >= least ? count_of(key) : 0;
+    const u64 w = c ? weight(x) : 0;
+    u64 mass = c * w;
+    uint32_t count = c;
+    mass = wave_scan(mass);
+    count = wave_scan(count);
+    mass += s.f_mass;
+    count += s.f_count;
+    const int at = __builtin_ctzll(__ballot(by_mass ? target <= mass : target <= count) | u64(1) << 63);
+    const u64 after = lane_value(mass, at), wf = lane_value(w, at);
+    Found f;
+    f.key = lane_value(key, at);
+    f.count = lane_value(c, at);
+    const u64 before = after - f.count * wf;
+    f.nth = by_mass ? uint32_t((target - before - 1) / (wf ? wf : 1)) : uint32_t(target - 1) - (lane_value(count, at) - f.count);
+    f.mass = before + u64(f.nth + 1) * wf;
+    __syncthreads();                      // everybody has read what the next search writes
+    return f;
+  };
+  u64 total = s.total;
+  if (set.top_k > 0 && uint32_t(set.top_k) < s.n) total = find(u64(set.top_k), false).mass;
+  if (set.top_p < 1.f) total = find(top_p_target(set.top_p, total), true).mass;
+  Found f = find(draw_target(set.u, total), true);
+  bool several = f.count > 1;
+  if (f.key == kZero16 || f.key == kMinusZero16) {
+    const uint32_t plus = count_of(kZero16);
+    if (f.key == kMinusZero16) f.nth += plus;
+    several = plus + count_of(kMinusZero16) > 1;
+  }
+  const int32_t token = index_of(f.key, f.nth, several);
+  if (tid == 0) write_result(a, r, token, key16_value(f.key), weight, set.temperature, total);
+  return true;
+}
+
+// Out of line: its registers are none of the path that rows take.
+__attribute__((noinline)) __device__ void sample_again(const SampleArgs &a, int64_t r, SampleLds &s) { sample_general<__bf16>(a, r, s); }
+
+template <int NV>
+__global__ __launch_bounds__(kSampleThreads) void sample_bf16_kernel(SampleArgs a) {
+  __shared__ union { CountLds counts; SampleLds general; } s;
+  if (sample_counts<NV, (NV <= 7)>(a, blockIdx.x, s.counts)) return;
+  if constexpr (NV > 7) {                         // no count of a shorter row overflows
+    __syncthreads();
+    sample_again(a, blockIdx.x, s.general);
   }
 }
 
@@ -344,8 +734,13 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
 
 hipError_t launch_sample(const SampleArgs &a, sp_dtype dtype, int64_t n_rows, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(n_rows)), block(kSampleThreads);
-  if (dtype == SP_BF16) hipLaunchKernelGGL(sample_kernel<__bf16>, grid, block, 0, s, a);
-  else hipLaunchKernelGGL(sample_kernel<float>, grid, block, 0, s, a);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
+  const int64_t nv = (a.vocab + 8 * kSampleThreads - 1) / (8 * kSampleThreads);
+  if (dtype == SP_F32) go(sample_f32_kernel);
+  else if (nv <= 4) go(sample_bf16_kernel<4>);
+  else if (nv <= 7) go(sample_bf16_kernel<7>);
+  else if (nv <= 16) go(sample_bf16_kernel<16>);
+  else go(sample_bf16_long_kernel);
   return hipGetLastError();
 }
 
