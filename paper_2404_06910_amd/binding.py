@@ -122,14 +122,28 @@ def _dev(t, what: str) -> int:
     return t.data_ptr()
 
 
-# These are called for every small table of every token and layer: one expression where all is well, and what was wrong is found
-# out only where something is.
-def _table_dev(t, what: str, dtype, n: Optional[int]):
-    """Device pointer of a contiguous tensor of one 32-bit type (and size); None -> NULL."""
+# Device pointers of contiguous tensors of one 32-bit type (and size), None -> NULL.  They are asked for every small table of every token
+# and layer: one expression where all is well, and what was wrong is found out only where something is.
+_I32 = _F32 = None
+
+
+def _i32_dev(t, what: str, n: Optional[int] = None):
     if t is None:
         return None
-    if t.dtype is dtype and t.is_cuda and t.is_contiguous() and (n is None or t.numel() == n):
+    if t.dtype is _I32 and t.is_cuda and t.is_contiguous() and (n is None or t.numel() == n):
         return t.data_ptr()
+    return _table_dev(t, what, _torch().int32, n)
+
+
+def _f32_dev(t, what: str, n: Optional[int] = None):
+    if t is None:
+        return None
+    if t.dtype is _F32 and t.is_cuda and t.is_contiguous() and (n is None or t.numel() == n):
+        return t.data_ptr()
+    return _table_dev(t, what, _torch().float32, n)
+
+
+def _table_dev(t, what: str, dtype, n: Optional[int]):
     if t.dtype is not dtype or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor" % (what, dtype))
     if n is not None and t.numel() != n:
@@ -137,23 +151,15 @@ def _table_dev(t, what: str, dtype, n: Optional[int]):
     return _dev(t, what)
 
 
-def _i32_dev(t, what: str, n: Optional[int] = None):
-    return None if t is None else _table_dev(t, what, _torch().int32, n)
-
-
-def _f32_dev(t, what: str, n: Optional[int] = None):
-    return None if t is None else _table_dev(t, what, _torch().float32, n)
-
-
 _TORCH = None
 
 
 def _torch():
     """torch, imported at its first use: host-only plans do without."""
-    global _TORCH
+    global _TORCH, _I32, _F32
     if _TORCH is None:
         import torch
-        _TORCH = torch
+        _TORCH, _I32, _F32 = torch, torch.int32, torch.float32
     return _TORCH
 
 
@@ -321,21 +327,23 @@ class Context:
                        n_nodes=None, resp_len=None, resp_len_add: int = 0, pos_resp=None):
         """K_resp, V_resp: [n_layers,] n_prompts, resp_capacity, n_kv_heads, head_dim, every layer's block contiguous."""
         B, N = draft.shape
-        if K_resp.dim() not in (4, 5) or K_resp.shape[-4] != B or V_resp.shape != K_resp.shape or V_resp.stride() != K_resp.stride():
+        shape, st = K_resp.shape, K_resp.stride()
+        if len(shape) not in (4, 5) or shape[-4] != B or V_resp.shape != shape or V_resp.stride() != st:
             raise ValueError("K_resp and V_resp must be alike, [n_layers,] n_prompts, resp_capacity, n_kv_heads, head_dim")
-        block = K_resp[0] if K_resp.dim() == 5 else K_resp
-        if not block.is_contiguous():
+        cap, heads, d = shape[-3:]
+        if st[-4:] != (cap * heads * d, heads * d, d, 1):
             raise ValueError("a layer's block of K_resp and V_resp must be contiguous")
-        if _dtype_code(V_resp) != _dtype_code(K_resp):
+        if V_resp.dtype is not K_resp.dtype:
             raise ValueError("K_resp and V_resp must have one dtype")
-        layers, stride = (K_resp.shape[0], K_resp.stride(0)) if K_resp.dim() == 5 else (1, 0)
-        cap, heads, d = block.shape[1:]
-        self._check(lib().sp_tree_accept(
+        layers, stride = (shape[0], st[0]) if len(shape) == 5 else (1, 0)
+        done = lib().sp_tree_accept(
             self._h, B, N, _i32_dev(parent, "parent", B * N), _i32_dev(n_nodes, "n_nodes", B), _i32_dev(draft, "draft", B * N),
             _i32_dev(sampled, "sampled", B * N), _dtype_code(K_resp), layers, stride, heads, d, _dev(K_resp, "K_resp"),
             _dev(V_resp, "V_resp"), _f32_dev(pos_resp, "pos_resp", B * cap), cap, _i32_dev(resp_len, "resp_len", B),
             int(resp_len_add), _i32_dev(path, "path", B * N), _i32_dev(n_accepted, "n_accepted", B),
-            _i32_dev(next_token, "next_token", B), _i32_dev(resp_len_out, "resp_len_out", B)))
+            _i32_dev(next_token, "next_token", B), _i32_dev(resp_len_out, "resp_len_out", B))
+        if done != 0:
+            self._check(done)
         return path
 
 

@@ -6,6 +6,8 @@
 // len + j of the cache.  path ascends and path[j] >= j, so whoever owns a column of the rows may move them one after the
 // other (in batches, each read before it is written) and never overwrites a row that is still to be read.
 // Bound by latency: a tree's three tables, the walk, the rows.  Every workgroup walks by itself: a second launch would cost more.
+#include <algorithm>
+
 #include "sp_device.h"
 #include "sp_internal.h"
 
@@ -49,15 +51,15 @@ __device__ __forceinline__ void walk_tree(const AcceptArgs &a, int b, Walk &w) {
 
 }  // namespace
 
-// MOVE: blockIdx.x = prompt, y = (layer, K or V), z = block of columns.  Without it a workgroup per prompt writes the results
-// alone: where resp_len_out is resp_len itself they come behind the moves of all workgroups, which read resp_len.
+// MOVE: blockIdx.x = prompt, y = part of its columns (16 bytes of a row of a layer's K or V).  Without it a workgroup per prompt writes
+// the results alone: where resp_len_out is resp_len itself they come behind the moves of all workgroups, which read resp_len.
 template <bool MOVE, bool RESULTS>
 __global__ __launch_bounds__(kAcceptThreads) void accept_kernel(AcceptArgs a) {
   __shared__ Walk w;
   const int b = blockIdx.x;
   if (threadIdx.x < 64) walk_tree(a, b, w);
   __syncthreads();
-  if (RESULTS && blockIdx.y == 0 && blockIdx.z == 0) {
+  if (RESULTS && blockIdx.y == 0) {
     if (int(threadIdx.x) < a.max_nodes)
       a.path[int64_t(b) * a.max_nodes + threadIdx.x] = int(threadIdx.x) < w.n ? w.path[threadIdx.x] : -1;
     if (threadIdx.x == 0) {
@@ -67,30 +69,37 @@ __global__ __launch_bounds__(kAcceptThreads) void accept_kernel(AcceptArgs a) {
     }
   }
   if (!MOVE) return;
-  if (a.pos_resp && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0) {
+  if (a.pos_resp && blockIdx.y == 0 && threadIdx.x < 64) {    // all positions are read before the first is written
     float *pos = a.pos_resp + int64_t(b) * a.resp_capacity + w.len;
-    for (int j = 0; j < w.n; ++j) pos[j] = pos[w.path[j]];
+    const bool mine = int(threadIdx.x) < w.n;
+    const float x = mine ? pos[w.path[threadIdx.x]] : 0.f;
+    if (mine) pos[threadIdx.x] = x;
   }
   int first = 0;                                              // rows that stay where they are
   while (first < w.n && w.path[first] == first) ++first;
-  const int col = blockIdx.z * kAcceptThreads + threadIdx.x;
-  if (first == w.n || col >= a.row_bytes / 16) return;
-  char *base = static_cast<char *>(blockIdx.y & 1 ? a.Vr : a.Kr) + int64_t(blockIdx.y >> 1) * a.layer_bytes +
-               (int64_t(b) * a.resp_capacity + w.len) * a.row_bytes + int64_t(col) * 16;
-  for (int j0 = first; j0 < w.n; j0 += kMoveBatch) {
-    u32x4 v[kMoveBatch];
+  if (first == w.n) return;
+  const int per_layer = a.row_bytes / 16;
+  const int64_t columns = int64_t(2) * a.n_layers * per_layer, at = (int64_t(b) * a.resp_capacity + w.len) * a.row_bytes;
+  for (int64_t c = int64_t(blockIdx.y) * kAcceptThreads + threadIdx.x; c < columns; c += int64_t(gridDim.y) * kAcceptThreads) {
+    const int64_t block = c / per_layer;
+    char *base = static_cast<char *>(block & 1 ? a.Vr : a.Kr) + (block >> 1) * a.layer_bytes + at + (c - block * per_layer) * 16;
+    for (int j0 = first; j0 < w.n; j0 += kMoveBatch) {
+      u32x4 v[kMoveBatch];
 #pragma unroll
-    for (int j = 0; j < kMoveBatch; ++j)
-      if (j0 + j < w.n) v[j] = ld16(base + int64_t(w.path[j0 + j]) * a.row_bytes);
+      for (int j = 0; j < kMoveBatch; ++j)
+        if (j0 + j < w.n) v[j] = ld16(base + int64_t(w.path[j0 + j]) * a.row_bytes);
 #pragma unroll
-    for (int j = 0; j < kMoveBatch; ++j)
-      if (j0 + j < w.n) st16(base + int64_t(j0 + j) * a.row_bytes, v[j]);
+      for (int j = 0; j < kMoveBatch; ++j)
+        if (j0 + j < w.n) st16(base + int64_t(j0 + j) * a.row_bytes, v[j]);
+    }
   }
 }
 
-hipError_t launch_accept(const AcceptArgs &a, int32_t n_prompts, int32_t n_layers, hipStream_t s) {
-  const unsigned cols = unsigned((a.row_bytes / 16 + kAcceptThreads - 1) / kAcceptThreads);
-  const dim3 grid(unsigned(n_prompts), 2u * unsigned(n_layers), cols), block(kAcceptThreads);
+hipError_t launch_accept(const AcceptArgs &a, int32_t n_prompts, int n_cu, hipStream_t s) {
+  // as many workgroups as are resident together (eight to a compute unit): each walks the tree for itself
+  const int64_t columns = int64_t(2) * a.n_layers * (a.row_bytes / 16), most = (columns + kAcceptThreads - 1) / kAcceptThreads;
+  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(most, int64_t(8) * n_cu / n_prompts));
+  const dim3 grid(unsigned(n_prompts), unsigned(std::min<int64_t>(parts, 65535))), block(kAcceptThreads);
   if (a.resp_len_out != a.resp_len) {
     hipLaunchKernelGGL((accept_kernel<true, true>), grid, block, 0, s, a);
   } else {

@@ -1490,9 +1490,9 @@ extern "C" sp_status sp_tree_accept(sp_ctx *ctx, int32_t n_prompts, int32_t max_
     return fail(&ctx->err, SP_ERR_INVALID_ARG, "resp_len_out overlaps resp_len");
   SP_HIP(ctx, hipSetDevice(ctx->device));
   hipError_t e = sp::launch_accept(
-      sp::AcceptArgs{parent, n_nodes, draft, sampled, max_nodes, K_resp, V_resp, pos_resp, n_layers > 1 ? layer_stride * esz : 0,
+      sp::AcceptArgs{parent, n_nodes, draft, sampled, max_nodes, K_resp, V_resp, pos_resp, n_layers, n_layers > 1 ? layer_stride * esz : 0,
                      int32_t(row * esz), resp_capacity, resp_len, resp_len_add, path, n_accepted, next_token, resp_len_out},
-      n_prompts, n_layers, ctx->stream);
+      n_prompts, ctx->n_cu, ctx->stream);
   if (e != hipSuccess) return fail(&ctx->err, SP_ERR_HIP, "accept launch: %s", hipGetErrorString(e));
   return SP_OK;
 }

@@ -325,6 +325,7 @@ struct AcceptArgs {
   int32_t max_nodes;
   void *Kr, *Vr;
   float *pos_resp;
+  int32_t n_layers;
   int64_t layer_bytes;
   int32_t row_bytes;                    // of a token: all KV heads
   int32_t resp_capacity;
@@ -332,6 +333,6 @@ struct AcceptArgs {
   int32_t resp_len_add;
   int32_t *path, *n_accepted, *next_token, *resp_len_out;
 };
-hipError_t launch_accept(const AcceptArgs &a, int32_t n_prompts, int32_t n_layers, hipStream_t s);
+hipError_t launch_accept(const AcceptArgs &a, int32_t n_prompts, int n_cu, hipStream_t s);
 
 }  // namespace sp

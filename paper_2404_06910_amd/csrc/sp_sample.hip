@@ -24,6 +24,7 @@ namespace {
 constexpr int kSampleThreads = 1024;
 constexpr int kSampleWaves = kSampleThreads / 64;
 constexpr int kBinBits = 13, kBins = 1 << kBinBits;
+constexpr int kSortedList = 256;                // keys that top-k leaves, up to which they are sorted
 constexpr int kList = 2048;                     // keys of one bin that are searched in LDS
 constexpr uint32_t kNegInfKey = 0x007fffffu;    // value_key(-inf)
 
@@ -422,6 +423,44 @@ __device__ __forceinline__ void sample_general(const SampleArgs &a, int64_t r, S
         });
         __syncthreads();
         find.few = true;
+        if (s.n_kept <= kSortedList) {
+          // So few are sorted, each by the number that come before it (1.5 us), and every search is one comparison.
+          const uint32_t kept = s.n_kept, tid = threadIdx.x;
+          if (tid < kept) {
+            const u64 mine = s.kept[tid];
+            uint32_t rank = 0;
+#pragma unroll 8
+            for (uint32_t j = 0; j < kept; ++j) rank += s.kept[j] > mine;
+            s.list[rank] = mine;
+          }
+          __syncthreads();
+          const u64 mine = tid < min(kept, uint32_t(set.top_k)) ? s.list[tid] : 0;
+          const float x = key_value(uint32_t(mine >> 32));
+          const u64 w = mine ? find.weight(x) : 0;
+          u64 before = w;
+          uint32_t none = 0;
+          scan_before(s, before, none);
+          // the weight up to the token that reaches a target, and the token itself
+          auto reach = [&](u64 target) {
+            if (before < target && target <= before + w) {
+              s.place.mass = before + w;
+              s.found_key = uint32_t(mine >> 32);
+              s.found_index = ~uint32_t(mine);
+            }
+            __syncthreads();
+            const u64 mass = s.place.mass;
+            __syncthreads();
+            return mass;
+          };
+          if (tid == kSampleThreads - 1) s.place.mass = before + w;
+          __syncthreads();
+          total = s.place.mass;
+          __syncthreads();
+          if (set.top_p < 1.f) total = reach(top_p_target(set.top_p, total));
+          reach(draw_target(set.u, total));
+          if (tid == 0) write_result(a, r, int32_t(s.found_index), key_value(s.found_key), find.weight, set.temperature, total);
+          return;
+        }
       }
     }
   }
