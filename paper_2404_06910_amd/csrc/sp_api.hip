@@ -1454,7 +1454,7 @@ extern "C" sp_status sp_sample(sp_ctx *ctx, const void *logits, sp_dtype dtype, 
     return fail(&ctx->err, SP_ERR_UNSUPPORTED, "logits base and row stride must be 16-byte aligned");
   SP_HIP(ctx, hipSetDevice(ctx->device));
   hipError_t e = sp::launch_sample(
-      sp::SampleArgs{logits, vocab, row_stride, rows_per_set, temperature, top_k, top_p, min_p, u, token, logprob}, dtype, n_rows,
+      sp::SampleArgs{logits, n_rows, vocab, row_stride, rows_per_set, temperature, top_k, top_p, min_p, u, token, logprob}, dtype,
       ctx->stream);
   if (e != hipSuccess) return fail(&ctx->err, SP_ERR_HIP, "sample launch: %s", hipGetErrorString(e));
   return SP_OK;

@@ -309,7 +309,7 @@ hipError_t launch_tree_decode(const sp_plan *plan, const TreeArgs &a, hipStream_
 
 struct SampleArgs {
   const void *logits;
-  int64_t vocab, row_stride;
+  int64_t n_rows, vocab, row_stride;
   int32_t rows_per_set;
   const float *temperature;
   const int32_t *top_k;
@@ -318,7 +318,7 @@ struct SampleArgs {
   float *logprob;
 };
 constexpr int64_t kSampleMaxVocab = int64_t(1) << 24;
-hipError_t launch_sample(const SampleArgs &a, sp_dtype dtype, int64_t n_rows, hipStream_t s);
+hipError_t launch_sample(const SampleArgs &a, sp_dtype dtype, hipStream_t s);
 
 struct AcceptArgs {
   const int32_t *parent, *n_nodes, *draft, *sampled;

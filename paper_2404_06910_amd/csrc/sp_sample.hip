@@ -14,6 +14,8 @@
 // One workgroup per row.  bf16 rows take counts alone: there are 65536 values, so a histogram of all of them in LDS is the sorted row, and a
 // weight is computed once per value that occurs, not per token (sample_counts).  fp32, and the bf16 rows that the 16-bit counts cannot
 // hold, build histograms of weights over the first 13 bits and go on inside a bin (RowSearch).
+#include <algorithm>
+
 #include "sp_device.h"
 #include "sp_internal.h"
 
@@ -327,7 +329,7 @@ struct Settings {
   int32_t top_k;
 };
 __device__ __forceinline__ Settings settings_of(const SampleArgs &a, int64_t r) {
-  const int64_t set = r / a.rows_per_set;
+  const uint32_t set = uint32_t(r) / uint32_t(a.rows_per_set);        // at most 2^30 rows
   return {a.temperature ? a.temperature[set] : 1.f, a.top_p ? a.top_p[set] : 1.f, a.min_p ? a.min_p[set] : 0.f,
           fminf(fmaxf(a.u[r], 0.f), 0x1.fffffep-1f), a.top_k ? a.top_k[set] : 0};      // u: NaN counts as 0
 }
@@ -508,36 +510,44 @@ struct CountLds {
   uint32_t f_group, f_count, n, counted, index, hits[16], wave_hits[kSampleWaves];
 };
 
-// A row of at most 8192 NV logits, NV vectors per thread, which stay in registers if there is room for them (KEEP) and are read
-// again, from the caches, when the token's index is looked for if not.  Returns false, having written nothing, if a value occurs too
-// often for a 16-bit count.
-template <int NV, bool KEEP>
-__device__ __forceinline__ bool sample_counts(const SampleArgs &a, int64_t r, CountLds &s) {
-  static_assert(KEEP || NV % 4 == 0, "read in fours");
-  constexpr uint32_t kPad = 0xff80ff80u;          // -inf
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int vocab = int(a.vocab), n_vec = (vocab + 7) / 8;
-  const uint16_t *row = static_cast<const uint16_t *>(a.logits) + r * a.row_stride;
-  auto load = [&](int i) {
-    const int at = i * kSampleThreads + tid;
+// A row of at most 8192 NV logits, NV vectors per thread.
+template <int NV>
+struct RowVectors {
+  static constexpr uint32_t kPad = 0xff80ff80u;   // -inf
+  const uint16_t *row;
+  int vocab;
+  u32x4 tail;                                     // the last, partial vector, in place of the padding that its thread has there
+  int tail_i;
+  __device__ __forceinline__ RowVectors(const SampleArgs &a, int64_t r)
+      : row(static_cast<const uint16_t *>(a.logits) + r * a.row_stride), vocab(int(a.vocab)), tail{kPad, kPad, kPad, kPad} {
+    tail_i = vocab % 8 && int(threadIdx.x) == vocab / 8 % kSampleThreads ? vocab / 8 / kSampleThreads : -1;
+    if (tail_i >= 0) {
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (e < vocab % 8) {
+          const uint32_t x = row[vocab / 8 * 8 + e];
+          tail[e / 2] = e & 1 ? (tail[e / 2] & 0xffffu) | x << 16 : (tail[e / 2] & 0xffff0000u) | x;
+        }
+    }
+  }
+  __device__ __forceinline__ u32x4 operator()(int i) const {
+    const int at = i * kSampleThreads + threadIdx.x;
     u32x4 x = {kPad, kPad, kPad, kPad};
     if (at < vocab / 8) x = ld16(row + int64_t(at) * 8);
     return x;
-  };
-  u32x4 tail = {kPad, kPad, kPad, kPad};          // the last, partial vector, in place of the padding that its thread has there
-  const int tail_i = vocab % 8 && tid == vocab / 8 % kSampleThreads ? vocab / 8 / kSampleThreads : -1;
-  if (tail_i >= 0) {
-#pragma unroll
-    for (int e = 0; e < 7; ++e)
-      if (e < vocab % 8) {
-        const uint32_t x = row[vocab / 8 * 8 + e];
-        tail[e / 2] = e & 1 ? (tail[e / 2] & 0xffffu) | x << 16 : (tail[e / 2] & 0xffff0000u) | x;
-      }
   }
-  u32x4 v[KEEP ? NV : 1];
-  if constexpr (KEEP)
-#pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = load(i);
+};
+
+// The vectors of a row are in registers if there is room for them (KEEP: v), or are read when they are counted and again, from the caches,
+// when the token's index is looked for.  Returns false, having written nothing, if a value occurs too often for a 16-bit count.
+template <int NV, bool KEEP>
+__device__ __forceinline__ bool sample_counts(const SampleArgs &a, int64_t r, const RowVectors<NV> &load, const u32x4 (&v)[KEEP ? NV : 1],
+                                              CountLds &s) {
+  static_assert(KEEP || NV % 4 == 0, "read in fours");
+  constexpr uint32_t kPad = RowVectors<NV>::kPad;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int vocab = int(a.vocab), n_vec = (vocab + 7) / 8, tail_i = load.tail_i;
+  const u32x4 tail = load.tail;
   const Settings set = settings_of(a, r);
   fill_table(s.table);
 #pragma unroll
@@ -550,7 +560,8 @@ __device__ __forceinline__ bool sample_counts(const SampleArgs &a, int64_t r, Co
 
   // two keys of a word at once: all bits of a negative number flip, the sign of a positive one
   auto keys = [](uint32_t w) { const uint32_t sign = (w >> 15) & 0x00010001u; return w ^ ((sign << 16) - sign | 0x80008000u); };
-  uint32_t out = 0;                               // -inf, counted by themselves: their 16 bits may overflow
+  // -inf (padding, masked tokens: often most of a row) is no value, and its atomics would all be one after the other
+  uint32_t out = 0;
   const bool may_overflow = NV > 7 && n_vec * 8 > 65535;
   // fn(vector, i) for all vectors of the thread; read from memory, four in flight
   auto vectors = [&](auto &&fn) {
@@ -576,8 +587,8 @@ __device__ __forceinline__ bool sample_counts(const SampleArgs &a, int64_t r, Co
     for (int e = 0; e < 4; ++e) {
       const uint32_t k = keys(x[e]), lo = k & 0xffffu, hi = k >> 16;
       if (may_overflow) out += (lo == 0x7f) + (hi == 0x7f);
-      atomicAdd(&s.hist[lo >> 1], (lo & 1) * 0xffffu + 1);
-      atomicAdd(&s.hist[hi >> 1], (hi & 1) * 0xffffu + 1);
+      if (lo != 0x7f) atomicAdd(&s.hist[lo >> 1], (lo & 1) * 0xffffu + 1);
+      if (hi != 0x7f) atomicAdd(&s.hist[hi >> 1], (hi & 1) * 0xffffu + 1);
     }
   });
   __syncthreads();
@@ -587,8 +598,7 @@ __device__ __forceinline__ bool sample_counts(const SampleArgs &a, int64_t r, Co
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const int w0 = wave * 2048 + j * 256 + lane * 4;
-    u32x4 c = *reinterpret_cast<const u32x4 *>(&s.hist[w0]);
-    if (w0 == 0x7f / 2 / 4 * 4) c[0x7f / 2 % 4] &= 0xffffu;          // without -inf
+    const u32x4 c = *reinterpret_cast<const u32x4 *>(&s.hist[w0]);
     const u64 some = __ballot((c[0] | c[1] | c[2] | c[3]) != 0);
     if (lane == 0) s.flags[wave * 8 + j] = some;
     if (may_overflow)
@@ -690,11 +700,13 @@ __device__ __forceinline__ bool sample_counts(const SampleArgs &a, int64_t r, Co
       mine &= mine - 1;
       const uint32_t key = uint32_t(g) * 64 + lane;
       const float x = key16_value(key);
-      uint32_t c = key <= kLast16 && x >= least ? count_of(key) : 0;
-      u64 mass = c ? c * weight(x) : 0;
-      mass = wave_scan(mass);
-      c = wave_scan(c);
-      if (lane == 63) { s.g_mass[g] = mass; s.g_count[g] = c; }
+      const uint32_t c = key <= kLast16 && x >= least ? count_of(key) : 0;
+      const u64 mass = wave_scan(c * weight(x));
+      if (lane == 63) s.g_mass[g] = mass;
+      if (set.top_k > 0) {
+        const uint32_t n = wave_scan(c);
+        if (lane == 63) s.g_count[g] = n;
+      }
     }
   }
   __syncthreads();
@@ -736,7 +748,16 @@ __device__ __forceinline__ bool sample_counts(const SampleArgs &a, int64_t r, Co
     f.key = lane_value(key, at);
     f.count = lane_value(c, at);
     const u64 before = after - f.count * wf;
-    f.nth = by_mass ? uint32_t((target - before - 1) / (wf ? wf : 1)) : uint32_t(target - 1) - (lane_value(count, at) - f.count);
+    f.nth = 0;
+    if (!by_mass) {
+      f.nth = uint32_t(target - 1) - (lane_value(count, at) - f.count);
+    } else if (f.count > 1) {             // (target - before - 1) / wf, by a quotient in 64 bits and what it is off
+      const u64 rest = target - before - 1;
+      u64 n = u64(double(rest) / double(wf));
+      if (n * wf > rest) --n;
+      else if (rest - n * wf >= wf) ++n;
+      f.nth = uint32_t(n);
+    }
     f.mass = before + u64(f.nth + 1) * wf;
     __syncthreads();                      // everybody has read what the next search writes
     return f;
@@ -761,24 +782,34 @@ __attribute__((noinline)) __device__ void sample_again(const SampleArgs &a, int6
 
 template <int NV>
 __global__ __launch_bounds__(kSampleThreads) void sample_bf16_kernel(SampleArgs a) {
+  __shared__ CountLds s;
+  const RowVectors<NV> row(a, blockIdx.x);
+  u32x4 v[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) v[i] = row(i);
+  sample_counts<NV, true>(a, blockIdx.x, row, v, s);
+}
+
+template <int NV>
+__global__ __launch_bounds__(kSampleThreads) void sample_bf16_wide_kernel(SampleArgs a) {
   __shared__ union { CountLds counts; SampleLds general; } s;
-  if (sample_counts<NV, (NV <= 7)>(a, blockIdx.x, s.counts)) return;
-  if constexpr (NV > 7) {                         // no count of a shorter row overflows
-    __syncthreads();
-    sample_again(a, blockIdx.x, s.general);
-  }
+  const RowVectors<NV> row(a, blockIdx.x);
+  const u32x4 none[1] = {};
+  if (sample_counts<NV, false>(a, blockIdx.x, row, none, s.counts)) return;
+  __syncthreads();
+  sample_again(a, blockIdx.x, s.general);
 }
 
 }  // namespace
 
-hipError_t launch_sample(const SampleArgs &a, sp_dtype dtype, int64_t n_rows, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(n_rows)), block(kSampleThreads);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
+hipError_t launch_sample(const SampleArgs &a, sp_dtype dtype, hipStream_t s) {
+  const dim3 block(kSampleThreads);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned(a.n_rows)), block, 0, s, a); };
   const int64_t nv = (a.vocab + 8 * kSampleThreads - 1) / (8 * kSampleThreads);
   if (dtype == SP_F32) go(sample_f32_kernel);
   else if (nv <= 4) go(sample_bf16_kernel<4>);
   else if (nv <= 7) go(sample_bf16_kernel<7>);
-  else if (nv <= 16) go(sample_bf16_kernel<16>);
+  else if (nv <= 16) go(sample_bf16_wide_kernel<16>);
   else go(sample_bf16_long_kernel);
   return hipGetLastError();
 }
