@@ -26,7 +26,7 @@ struct NewKeys {
   int64_t stride;
 };
 
-// One thread per source follows the tables (kept -> path slot descriptor, which carries the first range), so the
+// One thread per source (the workgroup has min(k, kDecMaxRanges - 1) + 1 of them at least) follows the tables (kept -> path slot descriptor, which carries the first range), so the
 // dependent loads of all sources run side by side; a prefix over the sources puts the ranges in order.
 // Where no prompt has more than 64 paths, the descriptors of a prompt's paths lie at a fixed place (path_stride; upload_plan
 // says where not) and the first wave reads all of them while `kept` is on its way, and picks from its lanes: one memory latency less for every

@@ -700,12 +700,13 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void tree_kernel(PlanDev pd, TreeD
 // workgroups than that; four waves to share a stage once two would give more workgroups than compute units.
 //   fp32, 48 pairs of 890 keys, up to 48 / 192 rows: 1 row wave times 4 key groups 45 / 125, in 2 pieces 33 / 139; 4 row waves 116 / 122,
 //     in 5 pieces 52 / 79.  512 / 1024 pairs, up to 16 rows: 1 wave 128 / 168, 2 key groups 83 / 166, 4 87 / 177
+// The key table takes a thread per kept path and one for the shared part: above 63 kept paths never a single wave.
 // Lists are cut into pieces, of at least a step for every key group, where that leaves compute units without a workgroup (fp32
 // with four row waves, of which three workgroups are resident: without three).
 struct TreeShape {
   int rt, rw, ks, blocks, pieces;
 };
-static TreeShape tree_shape(const sp_plan *plan, int max_nodes, int64_t keys, int64_t part_rows, int n_cu) {
+static TreeShape tree_shape(const sp_plan *plan, int max_nodes, int k, int64_t keys, int64_t part_rows, int n_cu) {
   const int G = plan->n_q_heads / plan->n_kv_heads, rows = max_nodes * G;
   const int64_t pairs = int64_t(plan->n_prompts) * plan->n_kv_heads;
   TreeShape t{rows <= 16 ? 1 : 2, 1, 1, 1, 1};
@@ -718,7 +719,7 @@ static TreeShape tree_shape(const sp_plan *plan, int max_nodes, int64_t keys, in
     if (rows > 64 && wgs() > n_cu) t.rw = 4;
     const int64_t n = wgs();
     if (n <= n_cu) t.ks = t.rw == 4 ? 2 : 4;
-    else if (n <= 2 * n_cu && t.rw == 1) t.ks = 2;
+    else if (t.rw == 1 && (n <= 2 * n_cu || k > 63)) t.ks = 2;
   } else {
     t.rt = 1;
     if (rows > 64) t.rw = 4;
@@ -759,7 +760,7 @@ hipError_t launch_tree_decode(const sp_plan *plan, const TreeArgs &a, hipStream_
   const int64_t resp = int64_t(a.resp_len_add) + (a.resp_len ? a.resp_capacity / 2 : 0);
   const int64_t keys = plan->max_shared_keys + int64_t(a.k) * plan->max_path_keys + std::min<int64_t>(resp, a.resp_capacity);
   const int n_cu = plan->ctx->n_cu;
-  const TreeShape t = tree_shape(plan, a.max_nodes, keys, d.rows, n_cu);
+  const TreeShape t = tree_shape(plan, a.max_nodes, a.k, keys, d.rows, n_cu);
   *no_scratch = false;
   d.n_pieces = t.pieces;
   if (t.pieces > 1) {
