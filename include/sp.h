@@ -33,7 +33,11 @@
  *   to 256).  A launch that gets none (of the 257th stream or capture) gives the same bits, slower: one workgroup then
  *   does the pieces in turn.  The regions are given back with the plan's tables.  Hence: replays of one captured
  *   decode must not overlap each other; after sp_plan_update, a graph captured before must not run beside other decodes
- *   of the plan; and a stream must have finished its decodes before it is destroyed.
+ *   of the plan; and a stream must have finished its decodes before it is destroyed.  Launches of sp_tree_decode that cut
+ *   their key lists (a few prompts, long lists) use regions of the same kind, 16 MiB each, allocated when a stream or
+ *   capture first needs one and handed on to later plans; one that gets none is refused (SP_ERR_WORKSPACE).  How often it
+ *   cuts goes by the call's sizes (max_nodes, k, resp_capacity, the plan), so equal calls give equal bits; the same nodes
+ *   in a call of other sizes may round differently.
  */
 #ifndef SP_H_
 #define SP_H_
@@ -279,7 +283,7 @@ sp_status sp_tree_decode(sp_ctx *ctx, const sp_plan *plan, const int32_t *kept, 
  * (SP_ERR_UNSUPPORTED above).  u: DEVICE fp32 [n_rows], random numbers in [0, 1) from the caller (others are clamped to it,
  * NaN counts as 0).  temperature, top_p, min_p: DEVICE fp32 and top_k: DEVICE int32, one value for every rows_per_set
  * consecutive rows ([ceil(n_rows / rows_per_set)]: the settings of a prompt for all nodes of its tree), or NULL (T = 1,
- * filter off).  token: DEVICE int32 [n_rows]; logprob: DEVICE fp32 [n_rows] or NULL.
+ * filter off).  token: DEVICE int32 [n_rows]; logprob: DEVICE fp32 [n_rows] or NULL; they must not overlap an input.
  * Weights are added up as 62-bit integers, so equal calls give equal tokens; a token that weighs less than 2^-38 of the first
  * (2^-45 for 128256 tokens) may count as weightless.
  */
@@ -302,7 +306,8 @@ sp_status sp_sample(sp_ctx *ctx, const void *logits, sp_dtype dtype, int64_t n_r
  * them (negative: nothing).  parent, n_nodes, max_nodes: as in sp_tree_decode.  K_resp, V_resp: DEVICE, n_layers blocks
  * [n_prompts, resp_capacity, n_kv_heads, head_dim], layer_stride elements apart (at least a block; not read with one layer).
  * pos_resp: DEVICE fp32 [n_prompts, resp_capacity] or NULL.  resp_len: DEVICE int32 [n_prompts] or NULL (= zeros).
- * resp_len_out: DEVICE int32 [n_prompts], may be resp_len itself (one more, small, launch), not overlap it otherwise.
+ * resp_len_out: DEVICE int32 [n_prompts], may be resp_len itself (one more, small, launch).  No result overlaps an input otherwise,
+ * and K_resp is not V_resp (SP_ERR_INVALID_ARG).
  */
 sp_status sp_tree_accept(sp_ctx *ctx, int32_t n_prompts, int32_t max_nodes, const int32_t *parent, const int32_t *n_nodes,
                          const int32_t *draft, const int32_t *sampled, sp_dtype dtype, int32_t n_layers, int64_t layer_stride,

@@ -277,11 +277,17 @@ class Context:
         if ks != V_prefill.stride() or ks[-1] != 1:
             raise ValueError("K_prefill and V_prefill must share strides, inner stride 1")
         shape, new = q_new.shape, k_new.shape
-        if len(shape) != 4 or shape[0] != plan.n_prompts or o_out.shape != shape:
+        B, N = plan.n_prompts, shape[1] if len(shape) == 4 else 0
+        head = (plan.n_kv_heads, plan.head_dim)
+        if shape != (B, N, plan.n_q_heads, plan.head_dim) or o_out.shape != shape:
             raise ValueError("q_new and o_out must be [n_prompts, max_nodes, n_q_heads, head_dim]")
-        if len(new) != 4 or new[:2] != shape[:2] or v_new.shape != new:
+        if new != (B, N) + head or v_new.shape != new:
             raise ValueError("k_new and v_new must be [n_prompts, max_nodes, n_kv_heads, head_dim]")
-        B, N = shape[:2]
+        if K_prefill.shape != (plan.n_tokens,) + head or V_prefill.shape != K_prefill.shape:
+            raise ValueError("K_prefill and V_prefill must be [n_tokens, n_kv_heads, head_dim]")
+        k, cap = int(k), int(resp_capacity)
+        if K_resp.numel() < B * cap * head[0] * head[1] or V_resp.numel() < B * cap * head[0] * head[1]:
+            raise ValueError("K_resp and V_resp must hold [n_prompts, resp_capacity, n_kv_heads, head_dim]")
         dt = _torch().float32 if plan.dtype == SP_F32 else _torch().bfloat16
         if not (K_resp.is_contiguous() and V_resp.is_contiguous() and q_new.is_contiguous() and k_new.is_contiguous()
                 and v_new.is_contiguous() and o_out.is_contiguous() and K_prefill.is_cuda and V_prefill.is_cuda and K_resp.is_cuda
@@ -299,8 +305,8 @@ class Context:
             for t, n in named:
                 _dev(t, n)
         st = lib().sp_tree_decode(
-            self._h, plan._h, _i32_dev(kept, "kept"), int(k), K_prefill.data_ptr(), V_prefill.data_ptr(), ks[0], ks[1],
-            K_resp.data_ptr(), V_resp.data_ptr(), _f32_dev(pos_resp, "pos_resp"), int(resp_capacity),
+            self._h, plan._h, _i32_dev(kept, "kept", B * k), k, K_prefill.data_ptr(), V_prefill.data_ptr(), ks[0], ks[1],
+            K_resp.data_ptr(), V_resp.data_ptr(), _f32_dev(pos_resp, "pos_resp", B * cap), cap,
             _i32_dev(resp_len, "resp_len", B), int(resp_len_add), _i32_dev(parent, "parent", B * N),
             _i32_dev(n_nodes, "n_nodes", B), N, _f32_dev(new_pos, "new_pos", B * N), q_new.data_ptr(), k_new.data_ptr(),
             v_new.data_ptr(), o_out.data_ptr(), float(softmax_scale))
@@ -358,13 +364,13 @@ class Plan:
         self._h = C.c_void_p()
         self.ctx = ctx
         self.dtype = dtype
-        self.n_q_heads = n_q_heads
+        self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
         st = lib().sp_plan_create(ctx._h if ctx else None, C.byref(t), n_q_heads, n_kv_heads, head_dim, dtype,
                                   C.byref(self._h))
         del keep
         if st != 0:
             raise SpError(st, lib().sp_last_error(ctx._h if ctx else None).decode())
-        self.n_prompts = t.n_prompts
+        self.n_prompts, self.n_tokens = t.n_prompts, t.n_tokens
 
     def update(self, prompt_seg_off, seg_tok_start, seg_tok_len, seg_parent, seg_path, n_tokens: int, tok_pos=None,
                alibi_slopes=None, seg_cached=None):
@@ -375,7 +381,7 @@ class Plan:
         del keep
         if st != 0:
             raise SpError(st, lib().sp_last_error(self.ctx._h if self.ctx else None).decode())
-        self.n_prompts = t.n_prompts
+        self.n_prompts, self.n_tokens = t.n_prompts, t.n_tokens
 
     def close(self):
         if getattr(self, "_h", None) and self._h.value:

@@ -165,7 +165,10 @@ extern "C" sp_status sp_create(sp_ctx **out, int device, void *hip_stream) {
 static void ctx_unref(sp_ctx *ctx) {
   if (--ctx->refs) return;
   for (void *p : ctx->dec_chunks) (void)hipFree(p);
-  for (void *p : ctx->tree_free) (void)hipFree(p);
+  for (const sp_ctx::FreeTree &f : ctx->tree_free) {
+    (void)hipFree(f.block);
+    if (f.done) (void)hipEventDestroy(f.done);
+  }
   delete ctx;
 }
 
@@ -293,6 +296,48 @@ const sp::DecodeRegion *sp::decode_region(const sp_plan *p, hipStream_t s) {
   return region_of(p->dec_regions, who);
 }
 
+// A block that a plan gave back, if the launches that still used it then are over or come before what `who` enqueues.
+static void *free_tree_block(sp_ctx *ctx, const sp::DecodeRegion &who) {
+  hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;               // a query while something is captured: no part of it
+  if (ctx->tree_free.empty() || hipThreadExchangeStreamCaptureMode(&mode) != hipSuccess) return nullptr;
+  void *block = nullptr;
+  for (size_t i = ctx->tree_free.size(); i-- > 0 && !block;) {
+    const sp_ctx::FreeTree f = ctx->tree_free[i];
+    const bool behind = f.stream == who.stream && !who.capture && who.stream != hipStreamPerThread;
+    if (!behind && !(f.done && hipEventQuery(f.done) == hipSuccess)) continue;
+    if (f.done) (void)hipEventDestroy(f.done);
+    block = f.block;
+    ctx->tree_free.erase(ctx->tree_free.begin() + std::ptrdiff_t(i));
+  }
+  (void)hipGetLastError();                                               // "not ready"
+  (void)hipThreadExchangeStreamCaptureMode(&mode);
+  return block;
+}
+
+// The blocks of a plan that goes.
+static void give_back_tree_blocks(sp_ctx *ctx, const sp_plan *plan) {
+  if (plan->tree_blocks.empty()) return;
+  sp::DecodeRegion who{};
+  hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+  const bool may = !ctx->closed && execution_order(ctx->stream, &who) && !who.capture && hipSetDevice(ctx->device) == hipSuccess &&
+                   hipThreadExchangeStreamCaptureMode(&mode) == hipSuccess;
+  for (const sp::DecodeRegion &r : plan->tree_blocks) {
+    hipEvent_t done = nullptr;
+    if (may && hipEventCreateWithFlags(&done, hipEventDisableTiming) == hipSuccess && hipEventRecord(done, ctx->stream) != hipSuccess) {
+      (void)hipEventDestroy(done);
+      done = nullptr;
+    }
+    try {
+      ctx->tree_free.push_back({r.part, ctx->stream, done});
+    } catch (const std::bad_alloc &) {
+      (void)hipFree(r.part);                                             // waits for whoever uses it
+      if (done) (void)hipEventDestroy(done);
+    }
+  }
+  if (may) (void)hipThreadExchangeStreamCaptureMode(&mode);
+  (void)hipGetLastError();
+}
+
 const sp::DecodeRegion *sp::tree_region(const sp_plan *p, hipStream_t s) {
   DecodeRegion who{};
   if (!execution_order(s, &who)) return nullptr;
@@ -300,15 +345,11 @@ const sp::DecodeRegion *sp::tree_region(const sp_plan *p, hipStream_t s) {
   if (p->tree_blocks.size() >= size_t(kDecMaxRegions)) return nullptr;
   try {
     p->tree_blocks.reserve(p->tree_blocks.size() + 1);
-    p->ctx->tree_free.reserve(p->ctx->tree_free.size() + p->tree_blocks.size() + 1);    // what this plan will give back
   } catch (const std::bad_alloc &) {
     return nullptr;
   }
-  void *block = nullptr;
-  if (!p->ctx->tree_free.empty()) {
-    block = p->ctx->tree_free.back();
-    p->ctx->tree_free.pop_back();
-  } else if (!(block = zeroed_block(kTreePartBytes + kTreeCounters * sizeof(uint32_t), kTreePartBytes, kTreeCounters * sizeof(uint32_t)))) {
+  void *block = free_tree_block(p->ctx, who);
+  if (!block && !(block = zeroed_block(kTreePartBytes + kTreeCounters * sizeof(uint32_t), kTreePartBytes, kTreeCounters * sizeof(uint32_t)))) {
     (void)hipGetLastError();
     return nullptr;
   }
@@ -1116,7 +1157,7 @@ extern "C" void sp_plan_destroy(sp_plan *plan) {
   if (plan->dev_blob) give_back_block(ctx, plan->dev_blob, plan->dev_blob_bytes);
   drop_decode_blocks(ctx, plan);
   if (plan->dec_scratch) ctx->dec_free.push_back({plan->dec_scratch, plan->dec_scratch_bytes});
-  for (const sp::DecodeRegion &r : plan->tree_blocks) ctx->tree_free.push_back(r.part);
+  give_back_tree_blocks(ctx, plan);
   delete plan;
   if (ctx) ctx_unref(ctx);
 }
@@ -1452,6 +1493,18 @@ extern "C" sp_status sp_sample(sp_ctx *ctx, const void *logits, sp_dtype dtype, 
   const int64_t esz = dtype == SP_BF16 ? 2 : 4;
   if ((reinterpret_cast<uintptr_t>(logits) & 15) || (row_stride * esz) % 16)
     return fail(&ctx->err, SP_ERR_UNSUPPORTED, "logits base and row stride must be 16-byte aligned");
+  // a row's workgroup reads its settings and logits when others have written their tokens
+  const int64_t n_sets = (n_rows + rows_per_set - 1) / rows_per_set;
+  struct Input { const void *at; int64_t bytes; };
+  const Input in[] = {{temperature, 4 * n_sets}, {top_k, 4 * n_sets}, {top_p, 4 * n_sets}, {min_p, 4 * n_sets}, {u, 4 * n_rows},
+                      {logits, ((n_rows - 1) * row_stride + vocab) * esz}};
+  const void *out[] = {token, logprob};
+  for (const Input &i : in)
+    for (const void *o : out) {
+      const char *x = static_cast<const char *>(i.at), *y = static_cast<const char *>(o);
+      if (x && y && x < y + 4 * n_rows && y < x + i.bytes)
+        return fail(&ctx->err, SP_ERR_INVALID_ARG, "token or logprob overlaps an input");
+    }
   SP_HIP(ctx, hipSetDevice(ctx->device));
   hipError_t e = sp::launch_sample(
       sp::SampleArgs{logits, n_rows, vocab, row_stride, rows_per_set, temperature, top_k, top_p, min_p, u, token, logprob}, dtype,
@@ -1486,8 +1539,16 @@ extern "C" sp_status sp_tree_accept(sp_ctx *ctx, int32_t n_prompts, int32_t max_
     return fail(&ctx->err, SP_ERR_UNSUPPORTED, "layer_stride must be a multiple of %lld elements", (long long)align);
   if ((reinterpret_cast<uintptr_t>(K_resp) | reinterpret_cast<uintptr_t>(V_resp)) & 15)
     return fail(&ctx->err, SP_ERR_UNSUPPORTED, "K_resp, V_resp must be 16-byte aligned");
-  if (resp_len && resp_len != resp_len_out && resp_len < resp_len_out + n_prompts && resp_len_out < resp_len + n_prompts)
-    return fail(&ctx->err, SP_ERR_INVALID_ARG, "resp_len_out overlaps resp_len");
+  if (K_resp == V_resp) return fail(&ctx->err, SP_ERR_INVALID_ARG, "K_resp and V_resp are one");
+  // every workgroup walks for itself, so nothing that the walk reads may be written by another one
+  const int64_t nodes = int64_t(n_prompts) * max_nodes;
+  struct Table { const int32_t *at; int64_t n; };
+  const Table in[] = {{draft, nodes}, {sampled, nodes}, {parent, nodes}, {n_nodes, n_prompts}, {resp_len, n_prompts}};
+  const Table out[] = {{path, nodes}, {n_accepted, n_prompts}, {next_token, n_prompts}, {resp_len_out, n_prompts}};
+  for (const Table &o : out)
+    for (const Table &i : in)
+      if (i.at && i.at < o.at + o.n && o.at < i.at + i.n && !(o.at == resp_len_out && i.at == resp_len && i.at == o.at))
+        return fail(&ctx->err, SP_ERR_INVALID_ARG, "a result overlaps an input (resp_len_out alone may be resp_len)");
   SP_HIP(ctx, hipSetDevice(ctx->device));
   hipError_t e = sp::launch_accept(
       sp::AcceptArgs{parent, n_nodes, draft, sampled, max_nodes, K_resp, V_resp, pos_resp, n_layers, n_layers > 1 ? layer_stride * esz : 0,

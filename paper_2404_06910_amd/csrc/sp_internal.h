@@ -183,7 +183,10 @@ struct sp_ctx {
   char *dec_at = nullptr;
   size_t dec_left = 0;
   std::vector<std::pair<void *, size_t>> dec_free;
-  std::vector<void *> tree_free;            // scratch of the trees of plans that are gone, for the next ones
+  // Scratch of the trees of plans that are gone, for the next ones: `stream` was the context's when the plan went, and `done`, if
+  // there is one, is behind what was enqueued there.
+  struct FreeTree { void *block; hipStream_t stream; hipEvent_t done; };
+  std::vector<FreeTree> tree_free;
   int refs = 1;               // the context itself + every live plan made on it
   bool closed = false;        // sp_destroy was called; the struct lives on until the last plan is gone
 };

@@ -339,7 +339,7 @@ __device__ __forceinline__ Weights weights_of(float m, float temperature, int vo
 // least value that min-p leaves
 __device__ __forceinline__ float min_p_value(float m, float temperature, float min_p) {
   if (!(min_p > 0.f)) return -INFINITY;
-  if (min_p >= 1.f) return m;
+  if (min_p >= 1.f || m == INFINITY) return m;
   const double limit = double(m) + double(temperature) * log(double(min_p));
   const float f = float(limit);
   return double(f) < limit ? nextafterf(f, INFINITY) : f;

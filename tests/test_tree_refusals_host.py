@@ -28,7 +28,7 @@ def ctx():
 
 
 class _Plan:
-    _h, dtype, n_prompts = C.c_void_p(), B.SP_F32, 2
+    _h, dtype, n_prompts, n_tokens, n_q_heads, n_kv_heads, head_dim = C.c_void_p(), B.SP_F32, 2, 9, 4, 2, 64
 
 
 def test_binding_checks(ctx):
@@ -36,12 +36,14 @@ def test_binding_checks(ctx):
     kv, new, q = z(9, 2, 64), z(2, 3, 2, 64), z(2, 3, 4, 64)
     resp = z(2, 8, 2, 64)
 
-    def tree(K=kv, V=kv, q=q, k=new, v=new, o=q, **kw):
-        ctx.sp_tree_decode(_Plan, i(2, 1), 1, K, V, resp, resp.clone(), 8, q, k, v, o, 1.0, **kw)
+    def tree(K=kv, V=kv, q=q, k=new, v=new, o=q, cap=8, kept=i(2, 1), **kw):
+        ctx.sp_tree_decode(_Plan, kept, 1, K, V, resp, resp.clone(), cap, q, k, v, o, 1.0, **kw)
 
     for kw, word in ((dict(V=kv.transpose(0, 1)), "strides"), (dict(o=z(2, 3, 4, 32)), "o_out"), (dict(q=z(3, 3, 4, 64)), "n_prompts"),
                      (dict(k=z(2, 4, 2, 64)), "k_new"), (dict(q=q.transpose(1, 2).contiguous().transpose(1, 2)), "contiguous"),
-                     (dict(q=q.bfloat16(), o=q.bfloat16()), "dtype"), (dict(), "CUDA")):
+                     (dict(q=q.bfloat16(), o=q.bfloat16()), "dtype"), (dict(), "CUDA"),
+                     (dict(q=z(2, 3, 2, 64), o=z(2, 3, 2, 64)), "n_q_heads"), (dict(k=z(2, 3, 1, 64), v=z(2, 3, 1, 64)), "n_kv_heads"),
+                     (dict(K=kv[:8], V=kv[:8]), "n_tokens"), (dict(cap=9), "resp_capacity"), (dict(q=q[0], o=q[0]), "max_nodes")):
         with pytest.raises(ValueError, match=word):
             tree(**kw)
     with pytest.raises(ValueError, match="inner stride"):
