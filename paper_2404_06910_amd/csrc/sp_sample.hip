@@ -14,7 +14,7 @@
 // One workgroup per row.  bf16 rows take counts alone: there are 65536 values, so a histogram of all of them in LDS is the sorted row, and a
 // weight is computed once per value that occurs, not per token (sample_counts).  fp32, and the bf16 rows that the 16-bit counts cannot
 // hold, build histograms of weights over the first 13 bits and go on inside a bin (RowSearch).
-#include <algorithm>
+#include <type_traits>
 
 #include "sp_device.h"
 #include "sp_internal.h"
@@ -38,6 +38,7 @@ __device__ __forceinline__ uint32_t value_key(float x) {
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float((k >> 31) ? k & 0x7fffffffu : ~k); }
 
 typedef unsigned long long u64;
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
 // Place of the search in the order: what lies before the token, or bin, that was found, and what that holds.
 struct Place {
@@ -67,9 +68,8 @@ struct Weights {
   int s_bits;       // weights are multiples of 2^-s_bits
   const double *table;
   __device__ __forceinline__ u64 operator()(float x) const {
-    if (x == m) return u64(1) << s_bits;
-    const double z = (double(x) - double(m)) * inv_t;            // in 64ths of an octave
-    if (!(z > -64.0 * 64.0) || m == INFINITY) return 0;          // below 2^-64
+    // in 64ths of an octave; at m itself the weight is 2^s_bits, from -64 octaves on it is 0 (NaN, and what is not infinite beside infinity)
+    const double z = x == m ? 0.0 : fmax((double(x) - double(m)) * inv_t, -65.0 * 64.0);
     const double n = rint(z), r = (z - n) * (0.69314718055994530942 / 64.0);
     const int i = int(n);
     double p = fma(r, 1.0 / 120.0, 1.0 / 24.0);
@@ -116,11 +116,16 @@ __device__ __forceinline__ u64 dpp(u64 x) { return u64(dpp<CTRL, ROWS>(uint32_t(
 // Sum over the lanes up to this one: in the rows of 16 by shifts, then the last lanes of rows to the rows behind.  (Through LDS, by
 // shuffles, a scan of weights and counts takes three times as long, and a row is a chain of them.)
 template <class X>
-__device__ __forceinline__ X wave_scan(X x) {
+__device__ __forceinline__ X row_scan(X x) {
   x += dpp<0x111, 0xf>(x);                       // row_shr 1, 2, 4, 8
   x += dpp<0x112, 0xf>(x);
   x += dpp<0x114, 0xf>(x);
   x += dpp<0x118, 0xf>(x);
+  return x;
+}
+template <class X>
+__device__ __forceinline__ X wave_scan(X x) {
+  x = row_scan(x);
   x += dpp<0x142, 0xa>(x);                       // row_bcast 15, 31
   x += dpp<0x143, 0xc>(x);
   return x;
@@ -503,6 +508,7 @@ struct CountLds {
   uint32_t g_count[1024];
   u64 flags[128];                       // a byte per group: has it any token?
   u64 some[kSampleWaves];               // a bit per group
+  uint16_t groups[1024];                // those that have any, ascending
   u64 wave_mass[kSampleWaves];
   uint32_t wave_count[kSampleWaves];
   double table[64];
@@ -541,7 +547,7 @@ struct RowVectors {
 // The vectors of a row are in registers if there is room for them (KEEP: v), or are read when they are counted and again, from the caches,
 // when the token's index is looked for.  Returns false, having written nothing, if a value occurs too often for a 16-bit count.
 template <int NV, bool KEEP>
-__device__ __forceinline__ bool sample_counts(const SampleArgs &a, int64_t r, const RowVectors<NV> &load, const u32x4 (&v)[KEEP ? NV : 1],
+__device__ __forceinline__ bool sample_counts(const SampleArgs &a, int64_t r, const RowVectors<NV> &load, u32x4 (&v)[KEEP ? NV : 1],
                                               CountLds &s) {
   static_assert(KEEP || NV % 4 == 0, "read in fours");
   constexpr uint32_t kPad = RowVectors<NV>::kPad;
@@ -564,11 +570,12 @@ __device__ __forceinline__ bool sample_counts(const SampleArgs &a, int64_t r, co
   uint32_t out = 0;
   const bool may_overflow = NV > 7 && n_vec * 8 > 65535;
   // fn(vector, i) for all vectors of the thread; read from memory, four in flight
-  auto vectors = [&](auto &&fn) {
+  auto vectors = [&](auto first, auto &&fn) {
     if constexpr (KEEP) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        fn(i == tail_i ? tail : v[i], i);
+        if (decltype(first)::value) v[i] = i == tail_i ? tail : v[i];
+        fn(v[i], i);
         __builtin_amdgcn_sched_barrier(0);
       }
     } else {
@@ -582,7 +589,7 @@ __device__ __forceinline__ bool sample_counts(const SampleArgs &a, int64_t r, co
       }
     }
   };
-  vectors([&](const u32x4 &x, int) {
+  vectors(std::true_type{}, [&](const u32x4 &x, int) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const uint32_t k = keys(x[e]), lo = k & 0xffffu, hi = k >> 16;
@@ -613,24 +620,22 @@ __device__ __forceinline__ bool sample_counts(const SampleArgs &a, int64_t r, co
   __syncthreads();
   // (a count that overflows loses 65536, or loses it and adds one to its neighbour)
   if (may_overflow && s.counted != uint32_t(NV * kSampleThreads * 8)) return false;
-  {
-    const bool some = (s.flags[tid >> 3] >> (8 * (tid & 7)) & 0xff) != 0 && tid >= int(kFirst16 / 64) && tid <= int(kLast16 / 64);
-    const u64 b = __ballot(some);
-    if (lane == 0) s.some[wave] = b;
-  }
+  const bool some = (s.flags[tid >> 3] >> (8 * (tid & 7)) & 0xff) != 0 && tid >= int(kFirst16 / 64) && tid <= int(kLast16 / 64);
+  const u64 some_here = __ballot(some);
+  if (lane == 0) s.some[wave] = some_here;
+  __syncthreads();
+  const uint32_t groups_to = row_scan(uint32_t(__popcll(s.some[lane & (kSampleWaves - 1)])));
+  const int n_groups = int(lane_value(groups_to, kSampleWaves - 1));
+  if (some)
+    s.groups[(wave ? lane_value(groups_to, wave - 1) : 0) + uint32_t(__popcll(some_here & ((u64(1) << lane) - 1)))] = uint16_t(tid);
   __syncthreads();
   auto count_of = [&](uint32_t key) { return (s.hist[key >> 1] >> (16 * (key & 1))) & 0xffffu; };
   // the largest value
   uint32_t top = 0;
-  for (int w = kSampleWaves - 1; w >= 0 && top == 0; --w) {
-    u64 b = s.some[w];
-    while (b && top == 0) {
-      const int g = 63 - __builtin_clzll(b);
-      b &= ~(u64(1) << g);
-      const uint32_t key = uint32_t(w * 64 + g) * 64 + lane;
-      const u64 here = __ballot(key <= kLast16 && count_of(key) > 0);
-      if (here) top = uint32_t(w * 64 + g) * 64 + (63 - __builtin_clzll(here));
-    }
+  for (int i = n_groups - 1; i >= 0 && top == 0; --i) {
+    const uint32_t first = uint32_t(s.groups[i]) * 64, key = first + lane;
+    const u64 here = __ballot(key <= kLast16 && count_of(key) > 0);
+    if (here) top = first + (63 - __builtin_clzll(here));
   }
   const float m = key16_value(top);
 
@@ -647,8 +652,15 @@ __device__ __forceinline__ bool sample_counts(const SampleArgs &a, int64_t r, co
       }
       return h;
     };
-    vectors([&](const u32x4 &x, int i) {
-      if (const uint32_t h = hits(x)) {
+    auto any = [&](const u32x4 &x) {      // halves without a difference, found by the least of four words' halves
+      u16x2 least_of = {0xffff, 0xffff};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) least_of = __builtin_elementwise_min(least_of, __builtin_bit_cast(u16x2, (x[e] ^ pair) & mask));
+      return least_of[0] == 0 || least_of[1] == 0;
+    };
+    vectors(std::false_type{}, [&](const u32x4 &x, int i) {
+      if (any(x)) {
+        const uint32_t h = hits(x);
         if (several) atomicAdd(&s.hits[i], uint32_t(__popc(h)));
         else s.index = uint32_t(i * kSampleThreads + tid) * 8 + __ffs(h) - 1;
       }
@@ -692,21 +704,26 @@ __device__ __forceinline__ bool sample_counts(const SampleArgs &a, int64_t r, co
   const Weights weight = weights_of(m, set.temperature, vocab, s.table);
   const float least = min_p_value(m, set.temperature, set.min_p);
 
-  // weigh the groups that hold any: wave w takes every 16th
-  for (int b = 0; b < kSampleWaves; ++b) {
-    u64 mine = s.some[b] & (0x0001000100010001ull << wave);
-    while (mine) {
-      const int g = b * 64 + __builtin_ctzll(mine);
-      mine &= mine - 1;
-      const uint32_t key = uint32_t(g) * 64 + lane;
-      const float x = key16_value(key);
-      const uint32_t c = key <= kLast16 && x >= least ? count_of(key) : 0;
-      const u64 mass = wave_scan(c * weight(x));
-      if (lane == 63) s.g_mass[g] = mass;
-      if (set.top_k > 0) {
-        const uint32_t n = wave_scan(c);
-        if (lane == 63) s.g_count[g] = n;
-      }
+  // weigh the groups that hold any: a wave four at a time, sixteen lanes a group, four keys a lane
+  for (int i0 = wave * 4; i0 < n_groups; i0 += kSampleWaves * 4) {
+    const int i = i0 + (lane >> 4);
+    const uint32_t g = s.groups[min(i, n_groups - 1)], key0 = g * 64 + (lane & 15) * 4;
+    const uint2 counts = *reinterpret_cast<const uint2 *>(&s.hist[key0 >> 1]);
+    u64 mass = 0;
+    uint32_t n = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float x = key16_value(key0 + e);
+      uint32_t c = ((e < 2 ? counts.x : counts.y) >> (16 * (e & 1))) & 0xffffu;
+      if (key0 + e > kLast16 || !(x >= least)) c = 0;
+      mass += c * weight(c ? x : m);
+      n += c;
+    }
+    mass = row_scan(mass);
+    if ((lane & 15) == 15 && i < n_groups) s.g_mass[g] = mass;
+    if (set.top_k > 0) {
+      n = row_scan(n);
+      if ((lane & 15) == 15 && i < n_groups) s.g_count[g] = n;
     }
   }
   __syncthreads();
@@ -794,7 +811,7 @@ template <int NV>
 __global__ __launch_bounds__(kSampleThreads) void sample_bf16_wide_kernel(SampleArgs a) {
   __shared__ union { CountLds counts; SampleLds general; } s;
   const RowVectors<NV> row(a, blockIdx.x);
-  const u32x4 none[1] = {};
+  u32x4 none[1] = {};
   if (sample_counts<NV, false>(a, blockIdx.x, row, none, s.counts)) return;
   __syncthreads();
   sample_again(a, blockIdx.x, s.general);
