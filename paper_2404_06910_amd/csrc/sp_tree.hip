@@ -12,8 +12,8 @@
 //
 // Measured, us for one layer (bytes that have to move at a large copy's 5.1 TB/s: floor), bf16 unless said:
 //   64 prompts of 32 heads, 16 nodes, 2 kept paths     121.5 (floor 125): HBM, 5.2 TB/s
-//   16 prompts of 32/8 heads, 64 nodes, 950 keys        33.5 (17): 2048 rows to 256 workgroups, the steps' barriers and issue of products and exponents
-//   2 prompts of 32/4 heads of 64 dims, 33 nodes, up to 12000 keys   25.4 (3.6): a piece's chain of steps
+//   16 prompts of 32/8 heads, 64 nodes, 950 keys        38.3 (17): 2048 rows to 256 workgroups, the steps' barriers and issue of products and exponents
+//   2 prompts of 32/4 heads of 64 dims, 33 nodes, up to 12000 keys   27.9 (3.6): a piece's chain of steps
 //   6 prompts of 32/8 heads, 12 nodes, 890 keys, fp32 with positions 31.2 (8.8): fp32 matrix pipe, a piece's chain
 //   one prompt of 32 heads, 5 nodes                     10.8 (1.4): latencies (launch, tables, K and V, merge)
 #include <algorithm>
@@ -265,6 +265,11 @@ __device__ __forceinline__ void finish(const PlanDev &pd, const TreeDev &d, int 
     else merge(std::integral_constant<int, 2>{});
   }
 
+// bf16: what the second product sums is the weights times this.  The upper half of a weight (its bits cut off) leaves less than 2^-7 of it; with the
+// factor the rest is never zero either (2^-10 of the weight at least), so that an infinite V that a row sees stays infinite: zero times
+// infinity is NaN.  The sum of the weights is multiplied by the same factor at the end.
+constexpr float kWeightScale = 1.f + 0x1p-10f;
+
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 
 }  // namespace
@@ -274,8 +279,10 @@ __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x)
 //   S^T[key, row]  = K[key, :] . Q[row, :]         A = K (LDS), B = Q (registers)
 //   O^T[d, row]   += V^T[d, key] . P^T[key, row]   A = V (LDS, transpose reads), B = P as it is
 // In the accumulator lane L holds row L % 16 and keys 4 (L / 16) + i of each tile, which are bound to the k-slots that the lane feeds in
-// the second product.  P is rounded to bf16 there, as the output is (the sum of the weights is not); that is half a step of every weight, and the
-// result is as far off as two roundings of it instead of one.
+// the second product.  A weight goes into it as two bf16 numbers, its upper half and what that leaves (kWeightScale), so that it is off by at most
+// 2^-15 of itself, and the result by little more than its one rounding (1.7e-3 of the outputs' norm from 64 bits, as the rounding alone; with weights of
+// one bf16 number 2.3e-3).  The product more costs nothing where HBM bounds a launch (64 prompts 121.6 / 121.7 us), and 33.5 / 38.3 and 25.4 / 27.9
+// in the two cases above where issue does.
 // fp32, v_mfma_f32_16x16x4_f32, everything in 32 bits:
 //   S^T[key, row] = K[key, :] . Q[row, :]       slots bound to dims 16 i + 4 (L / 16) + e
 //   O^T[d, row]  += V^T[d, key] . P^T[key, row] slot L / 16 of product r bound to key 4 (L / 16) + r; rows of O^T to dims 64 h + 4 (L % 16) + c
@@ -492,7 +499,7 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void tree_kernel(PlanDev pd, TreeD
         mx[t] = largest(s[t]);
       }
     }
-    u32x4 pb[RT];                                    // weights as pairs of bf16
+    u32x4 pb[RT], pr[RT];                            // weights as pairs of bf16: upper halves, and the rest
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       if (!BIAS) mx[t] *= scale2;                    // scale2 > 0
@@ -513,8 +520,13 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void tree_kernel(PlanDev pd, TreeD
         for (int i = 0; i < 4; ++i) p[i] = fast_exp2(BIAS ? s[t][h][i] - m_run[t] : fmaf(s[t][h][i], scale2, -m_run[t]));
         ls[h] = (p[0] + p[1]) + (p[2] + p[3]);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-          pb[t][2 * h + i] = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(p[2 * i]), static_cast<__bf16>(p[2 * i + 1])});
+        for (int i = 0; i < 2; ++i) {
+          const float a = p[2 * i], b = p[2 * i + 1];
+          const uint32_t w = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+          pb[t][2 * h + i] = w;
+          pr[t][2 * h + i] = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(fmaf(a, kWeightScale, -bf16_lo(w))),
+                                                                 static_cast<__bf16>(fmaf(b, kWeightScale, -bf16_hi(w)))});
+        }
       }
       l_run[t] += ls[0] + ls[1];
     }
@@ -541,6 +553,10 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void tree_kernel(PlanDev pd, TreeD
         }
       }
     }
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int t = 0; t < RT; ++t) o[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[c], __builtin_bit_cast(bf16x8, pr[t]), o[t][c], 0, 0, 0);
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -680,7 +696,7 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void tree_kernel(PlanDev pd, TreeD
     slot = slot + 1 == NS ? 0 : slot + 1;
   }
 #pragma unroll
-  for (int t = 0; t < RT; ++t) l_run[t] = rows_sum(l_run[t]);
+  for (int t = 0; t < RT; ++t) l_run[t] = rows_sum(l_run[t]) * (kBf16 ? kWeightScale : 1.f);
   if constexpr (kBf16) {
     finish<T, D, RT, RW, KS>(pd, d, b, g, n, rows, m_run, l_run, o, reinterpret_cast<float *>(ring), [&](int c) { return 16 * c + 4 * q; });
   } else {
