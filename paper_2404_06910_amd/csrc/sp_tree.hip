@@ -62,10 +62,10 @@ template <typename T, int D>
 __device__ __forceinline__ void append_nodes(const PlanDev &pd, const TreeArgs &a, int b, int g, int row0, int n) {
   constexpr int EV = Elem<T>::kVec, LPK = D / EV;
   const int Hkv = pd.n_kv_heads;
-  if (row0 < 0) return;
+  if (row0 < 0 || row0 >= a.resp_capacity) return;           // before any sum: row0 + node passes 31 bits for the largest lengths
+  n = min(n, a.resp_capacity - row0);
   for (int i = threadIdx.x; i < n * LPK; i += blockDim.x) {
     const int node = i / LPK, sub = i % LPK, row = row0 + node;
-    if (row >= a.resp_capacity) continue;
     const int64_t to = (((int64_t)b * a.resp_capacity + row) * Hkv + g) * D + sub * EV;
     const int64_t from = (((int64_t)b * a.max_nodes + node) * Hkv + g) * D + sub * EV;
     st16(static_cast<T *>(a.Kr) + to, ld16(static_cast<const T *>(a.k_new) + from));
