@@ -419,6 +419,7 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void tree_kernel(PlanDev pd, TreeD
   // elements, take them out of the product and add them key by key where the weight is not zero: weight(t, i) is that of key
   // 4 (L / 16) + i of the keys from t0 on, dim(c, e) the place of o[t][c][e].
   auto add_infinite = [&](int t0, auto &&weight, auto &&dim) {
+    if (t0 >= n_total) return;                       // half a step behind the list (bf16): no key, and no weight but zero
     const int i0 = find.uniform(t0);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
