@@ -19,6 +19,7 @@
 // 1024 of 50432 63 (20); 96 fp32 rows of 50257, the best 50 and a nucleus of them, 25.5 (3.8).  A workgroup fills a compute unit's LDS, so a
 // row's phases follow each other: of 15 us the load takes 4, the counts' atomics 4 (random bins: bank conflicts), and the rest are
 // latencies of scans and barriers.
+#include <algorithm>
 #include <type_traits>
 
 #include "sp_device.h"
@@ -339,7 +340,7 @@ struct Settings {
   int32_t top_k;
 };
 __device__ __forceinline__ Settings settings_of(const SampleArgs &a, int64_t r) {
-  const uint32_t set = uint32_t(r) / uint32_t(a.rows_per_set);        // at most 2^30 rows
+  const uint32_t set = uint32_t(r) / uint32_t(a.rows_per_set);        // at most 2^21 rows
   return {a.temperature ? a.temperature[set] : 1.f, a.top_p ? a.top_p[set] : 1.f, a.min_p ? a.min_p[set] : 0.f,
           fminf(fmaxf(a.u[r], 0.f), 0x1.fffffep-1f), a.top_k ? a.top_k[set] : 0};      // u: NaN counts as 0
 }
@@ -825,8 +826,24 @@ __global__ __launch_bounds__(kSampleThreads) void sample_bf16_wide_kernel(Sample
 }  // namespace
 
 hipError_t launch_sample(const SampleArgs &a, sp_dtype dtype, hipStream_t s) {
-  const dim3 block(kSampleThreads);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned(a.n_rows)), block, 0, s, a); };
+  // A launch has fewer than 2^32 threads.  More rows go in several, each of whole sets of settings, or of a part of one set.
+  constexpr int64_t kMost = int64_t(1) << 21;
+  const int64_t per = a.rows_per_set, esz = dtype == SP_F32 ? 4 : 2;
+  auto go = [&](auto kernel) {
+    for (int64_t r = 0, n; r < a.n_rows; r += n) {
+      n = std::min(a.n_rows - r, per <= kMost ? kMost / per * per : std::min(kMost, per - r % per));
+      SampleArgs part = a;
+      part.logits = static_cast<const char *>(a.logits) + r * a.row_stride * esz;
+      part.u = a.u + r;
+      part.token = a.token + r;
+      if (a.logprob) part.logprob = a.logprob + r;
+      if (a.temperature) part.temperature = a.temperature + r / per;
+      if (a.top_k) part.top_k = a.top_k + r / per;
+      if (a.top_p) part.top_p = a.top_p + r / per;
+      if (a.min_p) part.min_p = a.min_p + r / per;
+      hipLaunchKernelGGL(kernel, dim3(unsigned(n)), dim3(kSampleThreads), 0, s, part);
+    }
+  };
   const int64_t nv = (a.vocab + 8 * kSampleThreads - 1) / (8 * kSampleThreads);
   if (dtype == SP_F32) go(sample_f32_kernel);
   else if (nv <= 4) go(sample_bf16_kernel<4>);
