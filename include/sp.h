@@ -257,8 +257,8 @@ sp_status sp_pruned_decode(sp_ctx *ctx, const sp_plan *plan, const int32_t *kept
  * dropped, not written.  The rows of nodes that are not there (i >= n_nodes[b]) are left as they are, in o_out too.
  * parent: DEVICE int32 [n_prompts, max_nodes], the node above each node, which comes before it; -1: none.  NULL: the node before
  *   (node 0: none).  Contract: -1 <= parent[i] < i; any other value is taken as -1.
- * n_nodes: DEVICE int32 [n_prompts] or NULL (= max_nodes); clamped to [0, max_nodes].  max_nodes: 1 to 64
- *   (SP_ERR_UNSUPPORTED above).
+ * n_nodes: DEVICE int32 [n_prompts] or NULL (= max_nodes); clamped to [0, max_nodes].  max_nodes: 1 to 64;
+ *   n_prompts * n_kv_heads below 2^23 (SP_ERR_UNSUPPORTED above).
  * new_pos: DEVICE fp32 [n_prompts, max_nodes]; q_new, o_out: DEVICE [n_prompts, max_nodes, n_q_heads, head_dim]; k_new, v_new:
  *   DEVICE [n_prompts, max_nodes, n_kv_heads, head_dim]; all contiguous.  The others as in sp_pruned_decode.
  */
@@ -302,6 +302,7 @@ sp_status sp_sample(sp_ctx *ctx, const void *logits, sp_dtype dtype, int64_t n_r
  * and row len_b + path[b, j] of the response caches (K, V of every layer, and pos_resp) moves to row len_b + j; rows from
  * resp_len_out[b] on hold nothing of use afterwards, those of other prompts and below len_b are untouched.
  * A node whose row lies beyond resp_capacity has no K/V and is not taken (nor is any behind it).
+ * n_prompts below 2^24, n_layers at most 32767, n_kv_heads at most 65535, max_nodes as in sp_tree_decode (SP_ERR_UNSUPPORTED above).
  * draft, sampled: DEVICE int32 [n_prompts, max_nodes], the nodes' own tokens (node 0's is not read) and what was sampled at
  * them (negative: nothing).  parent, n_nodes, max_nodes: as in sp_tree_decode.  K_resp, V_resp: DEVICE, n_layers blocks
  * [n_prompts, resp_capacity, n_kv_heads, head_dim], layer_stride elements apart (at least a block; not read with one layer).

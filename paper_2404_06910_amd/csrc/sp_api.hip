@@ -1463,6 +1463,8 @@ extern "C" sp_status sp_tree_decode(sp_ctx *ctx, const sp_plan *plan, const int3
     return fail(&ctx->err, SP_ERR_UNSUPPORTED, "%d nodes (limit %d)", max_nodes, sp::kMaxNodes);
   if (int64_t(plan->n_prompts) * max_nodes > INT32_MAX)
     return fail(&ctx->err, SP_ERR_UNSUPPORTED, "n_prompts * max_nodes does not fit 31 bits");
+  if (int64_t(plan->n_prompts) * plan->n_kv_heads >= int64_t(1) << 23)      // workgroups of up to 512 threads, less than 2^32 in all
+    return fail(&ctx->err, SP_ERR_UNSUPPORTED, "n_prompts * n_kv_heads is 2^23 or more");
   if (o_out == q_new || o_out == k_new || o_out == v_new)
     return fail(&ctx->err, SP_ERR_INVALID_ARG, "o_out must not alias an input");
   SP_HIP(ctx, hipSetDevice(ctx->device));
@@ -1530,6 +1532,7 @@ extern "C" sp_status sp_tree_accept(sp_ctx *ctx, int32_t n_prompts, int32_t max_
   if (head_dim != 64 && head_dim != 128) return fail(&ctx->err, SP_ERR_UNSUPPORTED, "head_dim %d (64 or 128)", head_dim);
   if (max_nodes > sp::kMaxNodes)
     return fail(&ctx->err, SP_ERR_UNSUPPORTED, "%d nodes (limit %d)", max_nodes, sp::kMaxNodes);
+  if (n_prompts >= 1 << 24) return fail(&ctx->err, SP_ERR_UNSUPPORTED, "n_prompts is 2^24 or more");      // as in sp_tree_decode
   if (n_layers > 32767 || n_kv_heads > 65535) return fail(&ctx->err, SP_ERR_UNSUPPORTED, "more than 32767 layers or 65535 KV heads");
   const int64_t esz = dtype == SP_BF16 ? 2 : 4, row = int64_t(n_kv_heads) * head_dim;
   const int64_t align = 16 / esz;
