@@ -260,7 +260,8 @@ sp_status sp_pruned_decode(sp_ctx *ctx, const sp_plan *plan, const int32_t *kept
  * n_nodes: DEVICE int32 [n_prompts] or NULL (= max_nodes); clamped to [0, max_nodes].  max_nodes: 1 to 64;
  *   n_prompts * n_kv_heads below 2^23 (SP_ERR_UNSUPPORTED above).
  * new_pos: DEVICE fp32 [n_prompts, max_nodes]; q_new, o_out: DEVICE [n_prompts, max_nodes, n_q_heads, head_dim]; k_new, v_new:
- *   DEVICE [n_prompts, max_nodes, n_kv_heads, head_dim]; all contiguous.  The others as in sp_pruned_decode.
+ *   DEVICE [n_prompts, max_nodes, n_kv_heads, head_dim]; all contiguous; o_out overlaps none of q_new,
+ *   k_new and v_new (SP_ERR_INVALID_ARG), nor the caches.  The others as in sp_pruned_decode.
  */
 sp_status sp_tree_decode(sp_ctx *ctx, const sp_plan *plan, const int32_t *kept, int32_t k, const void *K_prefill,
                          const void *V_prefill, int64_t kv_tok_stride, int64_t kv_head_stride, void *K_resp, void *V_resp,
@@ -283,7 +284,7 @@ sp_status sp_tree_decode(sp_ctx *ctx, const sp_plan *plan, const int32_t *kept, 
  * n_rows at most 2^30 (SP_ERR_UNSUPPORTED above).  u: DEVICE fp32 [n_rows], random numbers in [0, 1) from the caller (others are clamped to it,
  * NaN counts as 0).  temperature, top_p, min_p: DEVICE fp32 and top_k: DEVICE int32, one value for every rows_per_set
  * consecutive rows ([ceil(n_rows / rows_per_set)]: the settings of a prompt for all nodes of its tree), or NULL (T = 1,
- * filter off).  token: DEVICE int32 [n_rows]; logprob: DEVICE fp32 [n_rows] or NULL; they must not overlap an input.
+ * filter off).  token: DEVICE int32 [n_rows]; logprob: DEVICE fp32 [n_rows] or NULL; neither overlaps an input or the other.
  * Weights are added up as 62-bit integers, so equal calls give equal tokens; a token that weighs less than 2^-38 of the first
  * (2^-45 for 128256 tokens) may count as weightless.
  */
@@ -307,8 +308,8 @@ sp_status sp_sample(sp_ctx *ctx, const void *logits, sp_dtype dtype, int64_t n_r
  * them (negative: nothing).  parent, n_nodes, max_nodes: as in sp_tree_decode.  K_resp, V_resp: DEVICE, n_layers blocks
  * [n_prompts, resp_capacity, n_kv_heads, head_dim], layer_stride elements apart (at least a block; not read with one layer).
  * pos_resp: DEVICE fp32 [n_prompts, resp_capacity] or NULL.  resp_len: DEVICE int32 [n_prompts] or NULL (= zeros).
- * resp_len_out: DEVICE int32 [n_prompts], may be resp_len itself (one more, small, launch).  No result overlaps an input otherwise,
- * and K_resp is not V_resp (SP_ERR_INVALID_ARG).
+ * resp_len_out: DEVICE int32 [n_prompts], may be resp_len itself (one more, small, launch).  No result overlaps an input otherwise, or
+ * another result or pos_resp, and K_resp is not V_resp (SP_ERR_INVALID_ARG).
  */
 sp_status sp_tree_accept(sp_ctx *ctx, int32_t n_prompts, int32_t max_nodes, const int32_t *parent, const int32_t *n_nodes,
                          const int32_t *draft, const int32_t *sampled, sp_dtype dtype, int32_t n_layers, int64_t layer_stride,

@@ -1396,6 +1396,16 @@ extern "C" sp_status sp_prune_topk(sp_ctx *ctx, const float *score, const int32_
 // ---------------------------------------------------------------------------------------
 // a4 decode
 // ---------------------------------------------------------------------------------------
+// Memory that an argument names; none for NULL.
+struct Span {
+  const void *at;
+  int64_t bytes;
+};
+static bool overlap(const Span &a, const Span &b) {
+  const char *x = static_cast<const char *>(a.at), *y = static_cast<const char *>(b.at);
+  return x && y && x < y + b.bytes && y < x + a.bytes;
+}
+
 static sp_status check_decode_args(sp_ctx *ctx, const sp_plan *plan, const int32_t *kept, int32_t k, const void *K_prefill,
                                    const void *V_prefill, int64_t kv_tok_stride, int64_t kv_head_stride, const void *K_resp,
                                    const void *V_resp, const float *pos_resp, int32_t resp_capacity, int32_t resp_len_add,
@@ -1465,7 +1475,10 @@ extern "C" sp_status sp_tree_decode(sp_ctx *ctx, const sp_plan *plan, const int3
     return fail(&ctx->err, SP_ERR_UNSUPPORTED, "n_prompts * max_nodes does not fit 31 bits");
   if (int64_t(plan->n_prompts) * plan->n_kv_heads >= int64_t(1) << 23)      // workgroups of up to 512 threads, less than 2^32 in all
     return fail(&ctx->err, SP_ERR_UNSUPPORTED, "n_prompts * n_kv_heads is 2^23 or more");
-  if (o_out == q_new || o_out == k_new || o_out == v_new)
+  // workgroups read the nodes' rows when others have written their results
+  const int64_t head_bytes = int64_t(plan->n_prompts) * max_nodes * plan->head_dim * (plan->dtype == SP_BF16 ? 2 : 4);
+  const Span o{o_out, head_bytes * plan->n_q_heads}, q{q_new, o.bytes}, kn{k_new, head_bytes * plan->n_kv_heads}, vn{v_new, kn.bytes};
+  if (overlap(o, q) || overlap(o, kn) || overlap(o, vn))
     return fail(&ctx->err, SP_ERR_INVALID_ARG, "o_out must not alias an input");
   SP_HIP(ctx, hipSetDevice(ctx->device));
   bool no_scratch = false;
@@ -1497,16 +1510,12 @@ extern "C" sp_status sp_sample(sp_ctx *ctx, const void *logits, sp_dtype dtype, 
     return fail(&ctx->err, SP_ERR_UNSUPPORTED, "logits base and row stride must be 16-byte aligned");
   // a row's workgroup reads its settings and logits when others have written their tokens
   const int64_t n_sets = (n_rows + rows_per_set - 1) / rows_per_set;
-  struct Input { const void *at; int64_t bytes; };
-  const Input in[] = {{temperature, 4 * n_sets}, {top_k, 4 * n_sets}, {top_p, 4 * n_sets}, {min_p, 4 * n_sets}, {u, 4 * n_rows},
-                      {logits, ((n_rows - 1) * row_stride + vocab) * esz}};
-  const void *out[] = {token, logprob};
-  for (const Input &i : in)
-    for (const void *o : out) {
-      const char *x = static_cast<const char *>(i.at), *y = static_cast<const char *>(o);
-      if (x && y && x < y + 4 * n_rows && y < x + i.bytes)
-        return fail(&ctx->err, SP_ERR_INVALID_ARG, "token or logprob overlaps an input");
-    }
+  const Span in[] = {{temperature, 4 * n_sets}, {top_k, 4 * n_sets}, {top_p, 4 * n_sets}, {min_p, 4 * n_sets}, {u, 4 * n_rows},
+                     {logits, ((n_rows - 1) * row_stride + vocab) * esz}};
+  const Span tokens{token, 4 * n_rows}, logprobs{logprob, 4 * n_rows};
+  for (const Span &i : in)
+    if (overlap(i, tokens) || overlap(i, logprobs)) return fail(&ctx->err, SP_ERR_INVALID_ARG, "token or logprob overlaps an input");
+  if (overlap(tokens, logprobs)) return fail(&ctx->err, SP_ERR_INVALID_ARG, "token and logprob overlap");
   SP_HIP(ctx, hipSetDevice(ctx->device));
   hipError_t e = sp::launch_sample(
       sp::SampleArgs{logits, n_rows, vocab, row_stride, rows_per_set, temperature, top_k, top_p, min_p, u, token, logprob}, dtype,
@@ -1544,14 +1553,17 @@ extern "C" sp_status sp_tree_accept(sp_ctx *ctx, int32_t n_prompts, int32_t max_
     return fail(&ctx->err, SP_ERR_UNSUPPORTED, "K_resp, V_resp must be 16-byte aligned");
   if (K_resp == V_resp) return fail(&ctx->err, SP_ERR_INVALID_ARG, "K_resp and V_resp are one");
   // every workgroup walks for itself, so nothing that the walk reads may be written by another one
-  const int64_t nodes = int64_t(n_prompts) * max_nodes;
-  struct Table { const int32_t *at; int64_t n; };
-  const Table in[] = {{draft, nodes}, {sampled, nodes}, {parent, nodes}, {n_nodes, n_prompts}, {resp_len, n_prompts}};
-  const Table out[] = {{path, nodes}, {n_accepted, n_prompts}, {next_token, n_prompts}, {resp_len_out, n_prompts}};
-  for (const Table &o : out)
-    for (const Table &i : in)
-      if (i.at && i.at < o.at + o.n && o.at < i.at + i.n && !(o.at == resp_len_out && i.at == resp_len && i.at == o.at))
+  const int64_t per_node = 4 * int64_t(n_prompts) * max_nodes, per_prompt = 4 * int64_t(n_prompts);
+  const Span in[] = {{draft, per_node}, {sampled, per_node}, {parent, per_node}, {n_nodes, per_prompt}, {resp_len, per_prompt}};
+  const Span out[] = {{path, per_node}, {n_accepted, per_prompt}, {next_token, per_prompt}, {resp_len_out, per_prompt},
+                      {pos_resp, per_prompt * resp_capacity}};
+  for (const Span &o : out) {
+    for (const Span &i : in)
+      if (overlap(o, i) && !(o.at == resp_len_out && i.at == resp_len && i.at == o.at))
         return fail(&ctx->err, SP_ERR_INVALID_ARG, "a result overlaps an input (resp_len_out alone may be resp_len)");
+    for (const Span &p : out)
+      if (&o != &p && overlap(o, p)) return fail(&ctx->err, SP_ERR_INVALID_ARG, "results overlap");
+  }
   SP_HIP(ctx, hipSetDevice(ctx->device));
   hipError_t e = sp::launch_accept(
       sp::AcceptArgs{parent, n_nodes, draft, sampled, max_nodes, K_resp, V_resp, pos_resp, n_layers, n_layers > 1 ? layer_stride * esz : 0,
