@@ -280,9 +280,9 @@ sp_status sp_tree_decode(sp_ctx *ctx, const sp_plan *plan, const int32_t *kept, 
  * token[r] is the first token of the order at which the running weight exceeds u[r] times the weight of what is left;
  * logprob[r] the logarithm of its weight over that weight.  T <= 0 (or NaN): the first token of the order, logprob 0.
  * Logits that are -inf or NaN take no part; a row with no others gets token -1 and logprob -inf.  Beside +inf nothing else weighs.
- * logits: DEVICE [n_rows, vocab], row_stride in elements, dtype fp32 or bf16, base and rows 16-byte aligned; vocab at most 2^24,
- * n_rows at most 2^30 (SP_ERR_UNSUPPORTED above).  u: DEVICE fp32 [n_rows], random numbers in [0, 1) from the caller (others are clamped to it,
- * NaN counts as 0).  temperature, top_p, min_p: DEVICE fp32 and top_k: DEVICE int32, one value for every rows_per_set
+ * logits: DEVICE [n_rows, vocab], row_stride in elements (of one row it is not read), dtype fp32 or bf16, base and rows 16-byte
+ * aligned; vocab at most 2^24, n_rows at most 2^30 (SP_ERR_UNSUPPORTED above).  u: DEVICE fp32 [n_rows], random numbers in
+ * [0, 1) from the caller (others are clamped to it, NaN counts as 0).  temperature, top_p, min_p: DEVICE fp32 and top_k: DEVICE int32, one value for every rows_per_set
  * consecutive rows ([ceil(n_rows / rows_per_set)]: the settings of a prompt for all nodes of its tree), or NULL (T = 1,
  * filter off).  token: DEVICE int32 [n_rows]; logprob: DEVICE fp32 [n_rows] or NULL; neither overlaps an input or the other.
  * Weights are added up as 62-bit integers, so equal calls give equal tokens; a token that weighs less than 2^-38 of the first

@@ -1498,6 +1498,7 @@ extern "C" sp_status sp_sample(sp_ctx *ctx, const void *logits, sp_dtype dtype, 
                                int32_t rows_per_set, const float *temperature, const int32_t *top_k, const float *top_p,
                                const float *min_p, const float *u, int32_t *token, float *logprob) {
   if (!ctx) return fail(nullptr, SP_ERR_INVALID_ARG, "ctx is NULL");
+  if (n_rows == 1 && vocab <= sp::kSampleMaxVocab) row_stride = (vocab + 7) / 8 * 8;      // nothing lies a row further
   if (n_rows < 0 || vocab <= 0 || rows_per_set <= 0 || row_stride < vocab)
     return fail(&ctx->err, SP_ERR_INVALID_ARG, "bad sizes (n_rows >= 0, vocab > 0, rows_per_set > 0, row_stride >= vocab)");
   if (n_rows == 0) return SP_OK;
