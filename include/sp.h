@@ -34,8 +34,9 @@
  *   does the pieces in turn.  The regions are given back with the plan's tables.  Hence: replays of one captured
  *   decode must not overlap each other; after sp_plan_update, a graph captured before must not run beside other decodes
  *   of the plan; and a stream must have finished its decodes before it is destroyed.  Launches of sp_tree_decode that cut
- *   their key lists (a few prompts, long lists) use regions of the same kind, 16 MiB each, allocated when a stream or
- *   capture first needs one and handed on to later plans; one that gets none is refused (SP_ERR_WORKSPACE).  How often it
+ *   their key lists (a few prompts, long lists) use regions of the same kind, allocated when a stream or capture first
+ *   needs one or needs a larger one (256 KiB to 16 MiB, by what the launch sums up), kept until the plan goes and handed on
+ *   to later plans; a launch for which the device has no memory is refused (SP_ERR_WORKSPACE).  How often it
  *   cuts goes by the call's sizes (max_nodes, k, resp_capacity, the plan), so equal calls give equal bits; the same nodes
  *   in a call of other sizes may round differently.
  */

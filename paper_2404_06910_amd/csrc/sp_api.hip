@@ -269,10 +269,11 @@ static bool execution_order(hipStream_t s, sp::DecodeRegion *who) {
   return true;
 }
 
-// Of some regions the one that belongs to `who`, or one that is free and now does, or nullptr.
-static sp::DecodeRegion *region_of(std::vector<sp::DecodeRegion> &regions, const sp::DecodeRegion &who) {
+// Of some regions, if they hold `bytes`, the one that belongs to `who`, or one that is free and now does, or nullptr.
+static sp::DecodeRegion *region_of(std::vector<sp::DecodeRegion> &regions, const sp::DecodeRegion &who, size_t bytes = 0) {
   sp::DecodeRegion *unused = nullptr;
   for (sp::DecodeRegion &r : regions) {
+    if (r.bytes < bytes) continue;
     if (r.taken && r.stream == who.stream && r.capture == who.capture && r.thread == who.thread) return &r;
     if (!r.taken && !unused) unused = &r;
   }
@@ -296,22 +297,27 @@ const sp::DecodeRegion *sp::decode_region(const sp_plan *p, hipStream_t s) {
   return region_of(p->dec_regions, who);
 }
 
-// A block that a plan gave back, if the launches that still used it then are over or come before what `who` enqueues.
-static void *free_tree_block(sp_ctx *ctx, const sp::DecodeRegion &who) {
+// The smallest block of enough bytes that a plan gave back, if the launches that still used it then are over or come before what `who`
+// enqueues.
+static bool free_tree_block(sp_ctx *ctx, const sp::DecodeRegion &who, size_t bytes, sp_ctx::FreeTree *found) {
   hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;               // a query while something is captured: no part of it
-  if (ctx->tree_free.empty() || hipThreadExchangeStreamCaptureMode(&mode) != hipSuccess) return nullptr;
-  void *block = nullptr;
-  for (size_t i = ctx->tree_free.size(); i-- > 0 && !block;) {
-    const sp_ctx::FreeTree f = ctx->tree_free[i];
+  if (ctx->tree_free.empty() || hipThreadExchangeStreamCaptureMode(&mode) != hipSuccess) return false;
+  size_t best = ctx->tree_free.size();
+  for (size_t i = ctx->tree_free.size(); i-- > 0;) {
+    const sp_ctx::FreeTree &f = ctx->tree_free[i];
+    if (f.bytes < bytes || (best < ctx->tree_free.size() && f.bytes >= ctx->tree_free[best].bytes)) continue;
     const bool behind = f.stream == who.stream && !who.capture && who.stream != hipStreamPerThread;
-    if (!behind && !(f.done && hipEventQuery(f.done) == hipSuccess)) continue;
-    if (f.done) (void)hipEventDestroy(f.done);
-    block = f.block;
-    ctx->tree_free.erase(ctx->tree_free.begin() + std::ptrdiff_t(i));
+    if (behind || (f.done && hipEventQuery(f.done) == hipSuccess)) best = i;
+  }
+  const bool any = best < ctx->tree_free.size();
+  if (any) {
+    *found = ctx->tree_free[best];
+    if (found->done) (void)hipEventDestroy(found->done);
+    ctx->tree_free.erase(ctx->tree_free.begin() + std::ptrdiff_t(best));
   }
   (void)hipGetLastError();                                               // "not ready"
   (void)hipThreadExchangeStreamCaptureMode(&mode);
-  return block;
+  return any;
 }
 
 // The blocks of a plan that goes.
@@ -328,9 +334,9 @@ static void give_back_tree_blocks(sp_ctx *ctx, const sp_plan *plan) {
       done = nullptr;
     }
     try {
-      ctx->tree_free.push_back({r.part, ctx->stream, done});
+      ctx->tree_free.push_back({r.count, r.bytes, ctx->stream, done});    // a block begins with its counters
     } catch (const std::bad_alloc &) {
-      (void)hipFree(r.part);                                             // waits for whoever uses it
+      (void)hipFree(r.count);                                            // waits for whoever uses it
       if (done) (void)hipEventDestroy(done);
     }
   }
@@ -338,23 +344,24 @@ static void give_back_tree_blocks(sp_ctx *ctx, const sp_plan *plan) {
   (void)hipGetLastError();
 }
 
-const sp::DecodeRegion *sp::tree_region(const sp_plan *p, hipStream_t s) {
+const sp::DecodeRegion *sp::tree_region(const sp_plan *p, hipStream_t s, size_t part_bytes) {
+  constexpr size_t kCountBytes = kTreeCounters * sizeof(uint32_t);
   DecodeRegion who{};
   if (!execution_order(s, &who)) return nullptr;
-  if (const DecodeRegion *r = region_of(p->tree_blocks, who)) return r;
-  if (p->tree_blocks.size() >= size_t(kDecMaxRegions)) return nullptr;
+  if (const DecodeRegion *r = region_of(p->tree_blocks, who, part_bytes)) return r;
   try {
     p->tree_blocks.reserve(p->tree_blocks.size() + 1);
   } catch (const std::bad_alloc &) {
     return nullptr;
   }
-  void *block = free_tree_block(p->ctx, who);
-  if (!block && !(block = zeroed_block(kTreePartBytes + kTreeCounters * sizeof(uint32_t), kTreePartBytes, kTreeCounters * sizeof(uint32_t)))) {
+  sp_ctx::FreeTree block{nullptr, size_t(256) << 10, nullptr, nullptr};  // sizes are powers of two, so that blocks fit the next plan too
+  while (block.bytes < part_bytes) block.bytes *= 2;
+  if (!free_tree_block(p->ctx, who, part_bytes, &block) && !(block.block = zeroed_block(kCountBytes + block.bytes, 0, kCountBytes))) {
     (void)hipGetLastError();
     return nullptr;
   }
-  p->tree_blocks.push_back({block, reinterpret_cast<uint32_t *>(static_cast<char *>(block) + kTreePartBytes), who.stream, who.capture,
-                            who.thread, true});
+  p->tree_blocks.push_back({static_cast<char *>(block.block) + kCountBytes, static_cast<uint32_t *>(block.block), who.stream, who.capture,
+                            who.thread, true, block.bytes});
   return &p->tree_blocks.back();
 }
 

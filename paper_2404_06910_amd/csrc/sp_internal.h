@@ -58,6 +58,7 @@ struct DecodeRegion {
   hipStream_t stream;
   unsigned long long capture, thread;     // capture id + 1; number of the thread; else 0
   bool taken;
+  size_t bytes = 0;                       // of `part`, where regions of a plan differ (trees)
 };
 
 // A run of segments fused on the query side: child segments that are packed directly behind
@@ -185,7 +186,7 @@ struct sp_ctx {
   std::vector<std::pair<void *, size_t>> dec_free;
   // Scratch of the trees of plans that are gone, for the next ones: `stream` was the context's when the plan went, and `done`, if
   // there is one, is behind what was enqueued there.
-  struct FreeTree { void *block; hipStream_t stream; hipEvent_t done; };
+  struct FreeTree { void *block; size_t bytes; hipStream_t stream; hipEvent_t done; };
   std::vector<FreeTree> tree_free;
   int refs = 1;               // the context itself + every live plan made on it
   bool closed = false;        // sp_destroy was called; the struct lives on until the last plan is gone
@@ -232,8 +233,9 @@ struct sp_plan {
   size_t dec_scratch_bytes = 0;
   mutable std::vector<sp::DecodeRegion> dec_regions;
   mutable std::vector<std::pair<void *, size_t>> dec_blocks;
-  // Scratch of tree launches that are cut into pieces: a block per order of execution too, from the context's or new, kept
-  // over updates and given back to the context with the plan (counters behind the partial sums; every launch leaves them zero).
+  // Scratch of tree launches that are cut into pieces: blocks of an order of execution too (a larger one where a launch asks for
+  // more than the others hold), from the context's or new, kept over updates and given back to the context with the plan (counters,
+  // which every launch leaves zero, then the partial sums).
   mutable std::vector<sp::DecodeRegion> tree_blocks;
   // device copies (one allocation)
   void *dev_blob = nullptr;
@@ -305,8 +307,8 @@ struct TreeArgs {
 // What a launch whose key lists are cut into pieces has at most: partial sums, and arrival counters (zero between launches).
 constexpr size_t kTreePartBytes = size_t(16) << 20;
 constexpr int kTreeCounters = 2048;
-// A region of that size for a launch on stream s, or nullptr when there is none to be had.
-const DecodeRegion *tree_region(const sp_plan *plan, hipStream_t s);
+// A region for a launch on stream s with that many bytes of partial sums (of kTreePartBytes at most), or nullptr when there is no memory.
+const DecodeRegion *tree_region(const sp_plan *plan, hipStream_t s, size_t part_bytes);
 // *no_scratch: nothing was launched, because there was none.
 hipError_t launch_tree_decode(const sp_plan *plan, const TreeArgs &a, hipStream_t s, bool *no_scratch);
 

@@ -788,7 +788,7 @@ hipError_t launch_tree_decode(const sp_plan *plan, const TreeArgs &a, hipStream_
   *no_scratch = false;
   d.n_pieces = t.pieces;
   if (t.pieces > 1) {
-    const DecodeRegion *region = tree_region(plan, s);
+    const DecodeRegion *region = tree_region(plan, s, size_t(t.pieces) * size_t(d.rows) * size_t(plan->head_dim + 2) * 4);
     if (!region) { *no_scratch = true; return hipSuccess; }
     d.part = static_cast<float *>(region->part);
     d.count = region->count;
