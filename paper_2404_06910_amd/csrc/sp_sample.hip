@@ -15,7 +15,7 @@
 // weight is computed once per value that occurs, not per token (sample_counts).  fp32, and the bf16 rows that the 16-bit counts cannot
 // hold, build histograms of weights over the first 13 bits and go on inside a bin (RowSearch).
 //
-// Measured, us: one bf16 row of 50432 with top-p 14.9; 64 of 128256, each with filters of its own, 32.3 (reading them once: 3.2);
+// Measured, us: one bf16 row of 50432 with top-p 14.9; 64 of 128256, each with filters of its own, 29.0 (reading them once: 3.2);
 // 1024 of 50432 63 (20); 96 fp32 rows of 50257, the best 50 and a nucleus of them, 25.5 (3.8).  A workgroup fills a compute unit's LDS, so a
 // row's phases follow each other: of 15 us the load takes 4, the counts' atomics 4 (random bins: bank conflicts), and the rest are
 // latencies of scans and barriers.
@@ -800,8 +800,13 @@ __device__ __forceinline__ bool sample_counts(const SampleArgs &a, int64_t r, co
   return true;
 }
 
-// Out of line: its registers are none of the path that rows take.
-__attribute__((noinline)) __device__ void sample_again(const SampleArgs &a, int64_t r, SampleLds &s) { sample_general<__bf16>(a, r, s); }
+// Out of line: its registers are none of the path that rows take.  The arguments come in LDS: as a reference to the kernel's they were copied
+// to memory by every workgroup (64 rows of 128256 32.2 / 29.0 us, 1024 rows 150 / 127).
+struct AgainLds {
+  SampleLds general;
+  SampleArgs args;
+};
+__attribute__((noinline)) __device__ void sample_again(AgainLds &s, int64_t r) { sample_general<__bf16>(s.args, r, s.general); }
 
 template <int NV>
 __global__ __launch_bounds__(kSampleThreads) void sample_bf16_kernel(SampleArgs a) {
@@ -815,12 +820,14 @@ __global__ __launch_bounds__(kSampleThreads) void sample_bf16_kernel(SampleArgs 
 
 template <int NV>
 __global__ __launch_bounds__(kSampleThreads) void sample_bf16_wide_kernel(SampleArgs a) {
-  __shared__ union { CountLds counts; SampleLds general; } s;
+  __shared__ union { CountLds counts; AgainLds again; } s;
   const RowVectors<NV> row(a, blockIdx.x);
   u32x4 none[1] = {};
   if (sample_counts<NV, false>(a, blockIdx.x, row, none, s.counts)) return;
   __syncthreads();
-  sample_again(a, blockIdx.x, s.general);
+  if (threadIdx.x == 0) s.again.args = a;
+  __syncthreads();
+  sample_again(s.again, blockIdx.x);
 }
 
 }  // namespace
