@@ -296,7 +296,10 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void tree_kernel(PlanDev pd, TreeD
   constexpr int RPC = ROWB < 256 ? 256 / ROWB : 1;                            // rows per 256 bytes (all banks)
   constexpr int HALFB = STEP * ROWB, SLOTB = 2 * HALFB;
   constexpr int NI = STEP / RG;                  // DMA instructions per half
-  constexpr bool STREAM = RW == 1;               // one block of rows: nobody else reads these keys
+  // Keys that one workgroup reads (bf16; fp32 up to 16 rows) are not kept in the caches.  fp32 has up to four blocks of 16 rows to a key, and they gain
+  // from the hint all the same, or lose nothing.  us with / without it: 64 prompts of 32/8 heads, 16 rows 96 / 106; 32 prompts, 32 rows 90 / 96, 64 rows
+  // 140 / 139; 6 prompts, 48 rows 32.0 / 31.8.
+  constexpr bool STREAM = RW == 1;
   constexpr int RINGB = NS * SLOTB * KS;
   constexpr int MERGEB = (KS - 1) * RW * RT * 16 * (D + 4) * 4;
   constexpr int NQ = CPR / 4, NC = D / 16;       // 16-byte vectors of a row per lane; output vectors
