@@ -716,13 +716,13 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void tree_kernel(PlanDev pd, TreeD
   }
 }
 
-// How a launch is shared out, a function of the call's sizes alone.  Measured, bf16, 128 dims, us for one layer (~500 keys, 32 KV
-// heads; 950 keys with 8), by waves that take different keys / different rows:
-//   up to 16 rows to a KV head, 6 / 8 / 10 / 16 / 20 / 32 prompts: 1 wave 29 / 29 / 32 / 36 / 43 / 55, 2 key groups
-//     20 / 22 / 27 / 31 / 48 / 60, 4 key groups 18 / 20 / 32 / 39 / 50 / 73
-//   60 rows, 4 / 8 / 16 / 32 prompts: 2 row waves 31 / 33 / 46 / 89, times 2 key groups 27 / 30 / 63 / 127, times 4 21 / 26 / 58 / 112
-//   256 rows, 4 / 8 / 16 / 32 prompts of 8 KV heads: 2 row waves times 4 key groups 24 / 26 / 49 / 116, 4 times 2 31 / 32 / 35 / 76,
-//     4 row waves 39 / 39 / 41 / 60
+// How a launch is shared out, a function of the call's sizes alone.  Measured, bf16, 128 dims (64 dims take half the LDS, and the same rule), us for
+// one layer (~500 keys, 32 KV heads; 950 keys with 60 rows and more), by waves that take different keys / different rows:
+//   up to 16 rows to a KV head, 6 / 8 / 10 / 16 / 20 / 32 prompts: 1 wave 30 / 29 / 32 / 36 / 43 / 58, 2 key groups
+//     20 / 22 / 27 / 32 / 49 / 61, 4 key groups 19 / 21 / 33 / 39 / 51 / 73
+//   60 rows, 4 / 8 / 16 / 32 prompts: 2 row waves 45 / 48 / 72 / 121, times 2 key groups 34 / 41 / 66 / 127, times 4 29 / 39 / 76 / 146
+//   256 rows, 4 / 8 / 16 / 32 prompts of 8 KV heads: 2 row waves times 4 key groups 26 / 29 / 53 / 118, 4 times 2 31 / 35 / 39 / 82,
+//     4 row waves 34 / 43 / 44 / 69
 // Hence: as many key groups as leave a workgroup to every compute unit (their slots fill its LDS), none where there are more
 // workgroups than that; four waves to share a stage once two would give more workgroups than compute units.
 //   fp32, 48 pairs of 890 keys, up to 48 / 192 rows: 1 row wave times 4 key groups 45 / 125, in 2 pieces 33 / 139; 4 row waves 116 / 122,
