@@ -15,7 +15,7 @@
 //   16 prompts of 32/8 heads, 64 nodes, 950 keys        38.3 (17): 2048 rows to 256 workgroups, the steps' barriers and issue of products and exponents
 //   2 prompts of 32/4 heads of 64 dims, 33 nodes, up to 12000 keys   27.9 (3.6): a piece's chain of steps
 //   6 prompts of 32/8 heads, 12 nodes, 890 keys, fp32 with positions 31.2 (8.8): fp32 matrix pipe, a piece's chain
-//   one prompt of 32 heads, 5 nodes                     10.8 (1.4): latencies (launch, tables, K and V, merge)
+//   one prompt of 32 heads, 5 nodes                     11.1 (1.4): latencies (launch, tables, K and V, merge)
 #include <algorithm>
 #include <type_traits>
 
