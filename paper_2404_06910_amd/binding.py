@@ -337,7 +337,8 @@ class Context:
         if len(shape) not in (4, 5) or shape[-4] != B or V_resp.shape != shape or V_resp.stride() != st:
             raise ValueError("K_resp and V_resp must be alike, [n_layers,] n_prompts, resp_capacity, n_kv_heads, head_dim")
         cap, heads, d = shape[-3:]
-        if st[-4:] != (cap * heads * d, heads * d, d, 1):
+        # (the stride of an extent of 1 may be anything)
+        if st[-4:] != (cap * heads * d, heads * d, d, 1) and not (K_resp[0] if len(shape) == 5 else K_resp).is_contiguous():
             raise ValueError("a layer's block of K_resp and V_resp must be contiguous")
         if V_resp.dtype is not K_resp.dtype:
             raise ValueError("K_resp and V_resp must have one dtype")
